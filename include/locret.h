@@ -30,6 +30,9 @@
  *   kept_idx     [n_kv_heads][budget]       int32; the first n_keep entries of each row are valid
  *   W1           [d_in][d_hidden]           s
  *   W2           [d_hidden][n_kv_heads]     s
+ *
+ * The locret_paged_* entry points at the end serve many requests from one pool of pages and need no context; the
+ * conventions that differ for them are stated there.
  */
 #ifndef LOCRET_H
 #define LOCRET_H
@@ -236,6 +239,116 @@ int locret_cache_view_q4(const locret_ctx* ctx, const void** Kq, const void** Vq
 int locret_profile_mode(locret_ctx* ctx, int32_t mode);
 int locret_profile_enable(locret_ctx* ctx, int32_t max_calls);
 int locret_profile_read(locret_ctx* ctx, double* stage_ms, int32_t* n_calls);
+
+/* ---- many requests on one pool of pages ---------------------------------------------------------------------------
+ *
+ * After their prompts, requests are generated together.  Their keys and values lie in pages of one pool per layer, so that no
+ * request needs a contiguous cache:
+ *   K, V          [n_pages][n_kv_heads][page_size][head_dim]   s; keys already rotated to their positions
+ *   block_table   [n_req][max_pages] int32: page p of request r holds its units p * page_size ...; entries from
+ *                 ceil(length / page_size) on are never read
+ *   lens          [n_req] int32: units of every request in the cache
+ *   slot          page * page_size + place in the page, of one unit
+ * A serving step is locret_paged_plan, then for every layer locret_paged_append and locret_paged_decode (one new token a
+ * request) or locret_paged_prefill (ragged chunks).  The retained cache of a locret_ctx is moved into pages by
+ * locret_paged_append too: its K and V (locret_cache_view) are read with head strides, rotated to positions 0, 1, ...
+ *
+ * Conventions: those of the top of this file, except
+ *   - calls carry their configuration (HOST) and workspace, and no state is kept between them: calls on different streams
+ *     or threads are independent as long as they share neither workspace nor outputs.  Two captured graphs that may run
+ *     at the same time need a workspace each.  Nothing in a workspace has to survive between calls or start at zero.
+ *   - all calls may be captured into HIP graphs: lengths, tables and counts are read on the device at each replay.
+ *   - pointers to q, k, v, K, V, outputs, weights and the workspace (256 bytes) are aligned as above; those to int32
+ *     and double arrays to their element.
+ *   - n_req = 0 or T = 0 is a valid call.
+ *   - device data is bounded by the kernels: lengths are taken as at least 0 and at most max_pages * page_size, units of a
+ *     block-table entry outside 0 .. n_pages - 1 are not seen, slots outside the pool are not written.
+ *   - attention: what a query does not see does not reach its result, whatever is stored there (infinities and NaN included).
+ *     Values that are seen may be up to 2^64 in size before their sums can leave the range of float. */
+typedef struct {
+  int32_t n_q_heads;      /* h; h / n_kv_heads at most 128                                       */
+  int32_t n_kv_heads;     /* must divide n_q_heads                                               */
+  int32_t head_dim;       /* 32, 64, 96 or 128                                                   */
+  int32_t dtype;          /* LOCRET_F32 or LOCRET_BF16: type of q, k, v, out and the pool        */
+  int32_t page_size;      /* units of a page: 16, 32, 64, 128 or 256                             */
+  int32_t n_pages;        /* pages of the pool; n_pages * page_size < 2^31                       */
+  int32_t max_reqs;       /* largest n_req of any call, at most LOCRET_PAGED_MAX_REQS            */
+  int32_t max_pages;      /* row length of block_table; max_pages * page_size < 2^31             */
+  int32_t window;         /* 0: a query sees every unit up to its own.  Else the last `window` of those only, its own counted */
+  int32_t n_sink;         /* with a window: units that stay visible at the start of every request */
+  float   softmax_scale;  /* 0 selects 1/sqrt(head_dim)                                          */
+} locret_paged_config;
+#define LOCRET_PAGED_MAX_REQS 4096
+
+/* Bytes of device workspace (256-byte aligned) that locret_paged_decode and locret_paged_prefill take.  0 if the configuration is
+ * invalid. */
+size_t locret_paged_workspace_bytes(const locret_paged_config* cfg);
+
+/* The bookkeeping of one serving step, on the device.
+ * lens, n_new [n_req]: units in the cache and new tokens of every request; n_new < 0: the request is finished.
+ * block_table, free_pages [n_pages], n_free [1] (entries 0 .. n_free - 1 of free_pages are free): the pool's state.
+ *   1. finished requests, in their order, give their pages (in theirs) to the end of free_pages; their length becomes 0;
+ *   2. requests, in their order, get pages for their new tokens, each page taken from the end of what is then free and entered
+ *      in block_table.  A request whose row is too short (lens + n_new > max_pages * page_size) takes nothing.  From
+ *      the first request on whose pages, or whose tokens within max_tokens, are not there, none takes anything.
+ * Out: lens_out [n_req] and n_free_out [1] (may be lens and n_free themselves); block_table and free_pages in place; cu_new
+ *   [n_req + 1]: first token of every request in the step's packed token order (cu_new[r+1] - cu_new[r] is 0 where nothing
+ *   was given, a shorter step that the caller sees there); slots, positions [max_tokens]: of every token, -1 and 0 behind the
+ *   last one. */
+int locret_paged_plan(const locret_paged_config* cfg, int32_t n_req, const int32_t* lens, const int32_t* n_new, int32_t* lens_out,
+                      int32_t* block_table, int32_t* free_pages, const int32_t* n_free, int32_t* n_free_out, int32_t max_tokens,
+                      int32_t* cu_new, int32_t* slots, int32_t* positions, void* stream);
+
+/* How a rotary embedding's frequencies are scaled for contexts longer than the model's first one. */
+#define LOCRET_ROPE_PLAIN    0   /* f_i = theta^(-2i/rotary_dim)                                                     */
+#define LOCRET_ROPE_LINEAR   1   /* f_i / factor                                                                      */
+#define LOCRET_ROPE_BANDS    2   /* by wavelength w = 2 pi / f_i: below original/high f_i, above original/low f_i / factor, between
+                                    them mixed with the weight (original/w - low) / (high - low) of f_i            */
+#define LOCRET_ROPE_RAMP     3   /* by rotations r_i = original f_i / 2 pi: mixed by a ramp over i from the pair with r = high
+                                    (rounded down) to the one with r = low (rounded up); amplitude 0.1 ln(factor) + 1  */
+#define LOCRET_ROPE_FACTORS  4   /* f_i / factors[i]; amplitude sqrt(1 + ln(factor) / ln(original)), 1 if factor <= 1   */
+typedef struct {
+  int32_t scaling;        /* LOCRET_ROPE_*                                                       */
+  int32_t rotary_dim;     /* rotated dims, the first ones of a head: even, 2 .. 4096             */
+  double  theta;          /* base, > 1                                                           */
+  double  factor;         /* > 0; extension of the context (not for PLAIN)                       */
+  double  original;       /* first context length, > 1 (BANDS, RAMP, FACTORS)                    */
+  double  low, high;      /* BANDS, RAMP: bounds, 0 < low < high                                 */
+  const double* factors;  /* HOST [rotary_dim / 2], > 0 (FACTORS)                                */
+} locret_rope_config;
+/* Frequencies in radians a position, freq HOST [rotary_dim / 2], and the factor of cosines and sines (amplitude HOST).  Host-only. */
+int locret_rope_frequencies(const locret_rope_config* cfg, double* freq, float* amplitude);
+
+/* Queries and keys of T tokens on their way into attention and cache, in one pass:
+ *   x' = x / sqrt(mean(x^2) + eps) * weight     per head, where q_weight / k_weight (float [head_dim]) is not NULL;
+ *   the first rotary_dim dims rotated by positions[t] * freq[i] (angles reduced in 64 bits), cosines and sines times `amplitude`: pairs
+ *   (i, i + rotary_dim / 2), or (2i, 2i + 1) if `interleaved`;
+ *   queries to q_out [T][n_q_heads][head_dim], keys and (unchanged) values to the pool at slots[t].
+ * All in 32 bits, rounded once.  Slots of a call are distinct; tokens whose slot is outside the pool (-1: padding) leave their query only.
+ * rotary_dim  0 (freq and positions are not read) or a multiple of 16, at most head_dim
+ * strides     HOST, NULL for dense tensors, or elements between tokens and between heads: {q token, q head, k token, k head, v token,
+ *             v head}, at least 0 and multiples of 16 bytes
+ * q and q_out may be NULL together, k and v (and slots, K, V) too.  q_out may be q where q is dense. */
+int locret_paged_append(const locret_paged_config* cfg, int32_t T, const void* q, const void* k, const void* v, const int64_t* strides,
+                        const int32_t* positions, const int32_t* slots, const double* freq, int32_t rotary_dim,
+                        int32_t interleaved, float amplitude, const float* q_weight, const float* k_weight, float eps,
+                        void* q_out, void* K, void* V, void* stream);
+
+/* Attention of one token per request, the last of its lens[r] units (already appended):
+ * q, out [n_req][n_q_heads][head_dim]; lse float [n_req][n_q_heads] or NULL: log of the sum of the exponentials of the visible
+ * logits.  A request that sees nothing (length 0) gets zeros and lse -inf. */
+int locret_paged_decode(const locret_paged_config* cfg, int32_t n_req, const void* q, const void* K, const void* V,
+                        const int32_t* block_table, const int32_t* lens, void* out, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Causal attention of a ragged batch of chunks.  Request r's queries are tokens cu_new[r] .. cu_new[r+1] - 1 of q
+ * [T][n_q_heads][head_dim] and the last of its lens[r] units (already appended): token cu_new[r] + i stands at position
+ * lens[r] - (cu_new[r+1] - cu_new[r]) + i and sees the units up to there, in the window or among the sinks.  cu_new does not fall and
+ * is taken within 0 .. T.  Rows of out and lse (as above) that belong to no request stay as they were; rows that see
+ * nothing are zeros and -inf. */
+int locret_paged_prefill(const locret_paged_config* cfg, int32_t n_req, int32_t T, const void* q, const void* K, const void* V,
+                         const int32_t* block_table, const int32_t* lens, const int32_t* cu_new, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 void locret_destroy(locret_ctx* ctx);
 

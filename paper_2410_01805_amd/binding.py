@@ -25,6 +25,8 @@ EXPORTS = [
     "locret_score", "locret_decode_step", "locret_evict_compact", "locret_cache_len", "locret_tokens_seen", "locret_cache_view",
     "locret_destroy", "locret_strerror", "locret_profile_mode", "locret_profile_enable", "locret_profile_read",
     "locret_set_head_budgets", "locret_cache_lens", "locret_score_static", "locret_cache_view_q4",
+    "locret_paged_workspace_bytes", "locret_paged_plan", "locret_rope_frequencies", "locret_paged_append", "locret_paged_decode",
+    "locret_paged_prefill",
 ]
 LOCRET_PROF_STAGES = 5
 LOCRET_MAX_HEAD_BUDGETS = 64
@@ -36,6 +38,25 @@ class locret_config(C.Structure):
         ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("chunk_max", C.c_int32),
         ("budget", C.c_int32), ("d_hidden", C.c_int32), ("rh_kv_expand", C.c_int32), ("dtype", C.c_int32),
         ("rope_mode", C.c_int32), ("rope_theta", C.c_float), ("softmax_scale", C.c_float), ("kv_bits", C.c_int32),
+    ]
+
+
+class locret_paged_config(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_reqs", C.c_int32), ("max_pages", C.c_int32),
+        ("window", C.c_int32), ("n_sink", C.c_int32), ("softmax_scale", C.c_float),
+    ]
+
+
+LOCRET_PAGED_MAX_REQS = 4096
+LOCRET_ROPE_PLAIN, LOCRET_ROPE_LINEAR, LOCRET_ROPE_BANDS, LOCRET_ROPE_RAMP, LOCRET_ROPE_FACTORS = range(5)
+
+
+class locret_rope_config(C.Structure):
+    _fields_ = [
+        ("scaling", C.c_int32), ("rotary_dim", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+        ("original", C.c_double), ("low", C.c_double), ("high", C.c_double), ("factors", C.POINTER(C.c_double)),
     ]
 
 
@@ -81,6 +102,20 @@ def _load() -> C.CDLL:
     lib.locret_cache_view_q4.restype = C.c_int
     lib.locret_cache_view_q4.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(i32), C.POINTER(i32),
                                          C.POINTER(i32), C.POINTER(i32)]
+    cfg = C.POINTER(locret_paged_config)
+    lib.locret_paged_workspace_bytes.restype = C.c_size_t
+    lib.locret_paged_workspace_bytes.argtypes = [cfg]
+    lib.locret_paged_plan.restype = C.c_int
+    lib.locret_paged_plan.argtypes = [cfg, i32] + [vp] * 7 + [i32] + [vp] * 4
+    lib.locret_rope_frequencies.restype = C.c_int
+    lib.locret_rope_frequencies.argtypes = [C.POINTER(locret_rope_config), C.POINTER(C.c_double), C.POINTER(C.c_float)]
+    lib.locret_paged_append.restype = C.c_int
+    lib.locret_paged_append.argtypes = [cfg, i32, vp, vp, vp, C.POINTER(C.c_int64), vp, vp, vp, i32, i32, C.c_float, vp, vp,
+                                        C.c_float, vp, vp, vp, vp]
+    lib.locret_paged_decode.restype = C.c_int
+    lib.locret_paged_decode.argtypes = [cfg, i32] + [vp] * 8 + [C.c_size_t, vp]
+    lib.locret_paged_prefill.restype = C.c_int
+    lib.locret_paged_prefill.argtypes = [cfg, i32, i32] + [vp] * 9 + [C.c_size_t, vp]
     lib.locret_profile_enable.restype = C.c_int
     lib.locret_profile_enable.argtypes = [vp, i32]
     lib.locret_profile_read.restype = C.c_int
@@ -238,6 +273,118 @@ def locret_destroy(ctx) -> None:
     lib.locret_destroy(ctx)
 
 
+# ---- many requests on one pool of pages ------------------------------------------------------------------------------
+# Tensors are checked against the configuration (type, density, size: LOCRET_EINVAL, LOCRET_ESHAPE), and the calls go to the device that
+# holds them, on that device's current stream unless one is given.  Addresses (ints) pass through unchecked.
+def _paged_tensor(where, t, dtype, numel, dense=True):
+    if t is None or isinstance(t, int):
+        return
+    if t.dtype != dtype or not t.is_cuda or (dense and not t.is_contiguous()):
+        raise LocretError(LOCRET_EINVAL, where)
+    if t.numel() < numel:
+        raise LocretError(LOCRET_ESHAPE, where)
+
+
+def _paged_call(where, fn, tensors, stream, *args):
+    devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
+    if len(devices) > 1:
+        raise LocretError(LOCRET_EINVAL, where)
+    with torch.cuda.device(devices.pop() if devices else None):
+        _check(fn(*args, _stream(stream)), where)
+
+
+def _paged_dtype(cfg):
+    return torch.bfloat16 if cfg.dtype == LOCRET_BF16 else torch.float32
+
+
+def _paged_pool(where, cfg, K, V):
+    n = cfg.n_pages * cfg.n_kv_heads * cfg.page_size * cfg.head_dim
+    _paged_tensor(where, K, _paged_dtype(cfg), n)
+    _paged_tensor(where, V, _paged_dtype(cfg), n)
+
+
+def locret_paged_workspace_bytes(cfg: locret_paged_config) -> int:
+    return lib.locret_paged_workspace_bytes(C.byref(cfg) if cfg is not None else None)
+
+
+def locret_paged_plan(cfg, n_req, lens, n_new, lens_out, block_table, free_pages, n_free, n_free_out, max_tokens, cu_new, slots, positions,
+                      stream=None) -> None:
+    where = "locret_paged_plan"
+    for t, n in ((lens, n_req), (n_new, n_req), (lens_out, n_req), (block_table, n_req * cfg.max_pages), (free_pages, cfg.n_pages), (n_free, 1),
+                 (n_free_out, 1), (cu_new, n_req + 1), (slots, max_tokens), (positions, max_tokens)):
+        _paged_tensor(where, t, torch.int32, n)
+    arrays = (lens, n_new, lens_out, block_table, free_pages, n_free, n_free_out, cu_new, slots, positions)
+    _paged_call(where, lib.locret_paged_plan, arrays, stream, C.byref(cfg), n_req, *map(_ptr, arrays[:7]), max_tokens, *map(_ptr, arrays[7:]))
+
+
+def locret_rope_frequencies(rotary_dim, theta, scaling=LOCRET_ROPE_PLAIN, factor=1.0, original=0.0, low=0.0, high=0.0, factors=None):
+    """(frequencies in radians a position, a list of rotary_dim / 2 floats; amplitude)."""
+    where = "locret_rope_frequencies"
+    if factors is not None and len(factors) != rotary_dim // 2:
+        raise LocretError(LOCRET_EINVAL, where)
+    arr = None if factors is None else (C.c_double * len(factors))(*[float(x) for x in factors])
+    cfg = locret_rope_config(scaling, rotary_dim, theta, factor, original, low, high, arr)
+    freq, amplitude = (C.c_double * max(1, rotary_dim // 2))(), C.c_float()
+    _check(lib.locret_rope_frequencies(C.byref(cfg), freq, C.byref(amplitude)), where)
+    return list(freq), amplitude.value
+
+
+def locret_paged_append(cfg, T, q, k, v, positions, slots, freq, rotary_dim, interleaved, amplitude, q_weight, k_weight, eps, q_out, K, V,
+                        stream=None, strides=None) -> None:
+    """q, k, v: [T][heads][head_dim] with any strides between tokens and heads (`strides` for addresses, see include/locret.h)."""
+    where = "locret_paged_append"
+    h, m, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    st = list(strides) if strides is not None else [h * d, d, m * d, d, m * d, d]
+    if len(st) != 6:
+        raise LocretError(LOCRET_EINVAL, where)
+    for i, (t, heads) in enumerate(((q, h), (k, m), (v, m))):
+        if t is None or isinstance(t, int):
+            continue
+        _paged_tensor(where, t, _paged_dtype(cfg), T * heads * d, dense=False)
+        if t.dim() != 3 or t.shape[0] < T or t.shape[1:] != (heads, d) or t.stride(2) != 1:
+            raise LocretError(LOCRET_ESHAPE, where)
+        st[2 * i: 2 * i + 2] = [t.stride(0), t.stride(1)] if strides is None else st[2 * i: 2 * i + 2]
+    _paged_tensor(where, q_out, _paged_dtype(cfg), T * h * d)
+    _paged_tensor(where, positions, torch.int32, T)
+    _paged_tensor(where, slots, torch.int32, T)
+    _paged_tensor(where, freq, torch.float64, rotary_dim // 2)
+    _paged_tensor(where, q_weight, torch.float32, d)
+    _paged_tensor(where, k_weight, torch.float32, d)
+    _paged_pool(where, cfg, K, V)
+    addr = lambda t: t.data_ptr() if torch.is_tensor(t) else t
+    _paged_call(where, lib.locret_paged_append, (q, k, v, positions, slots, freq, q_weight, k_weight, q_out, K, V), stream, C.byref(cfg), T, addr(q),
+                addr(k), addr(v), (C.c_int64 * 6)(*st), addr(positions), addr(slots), addr(freq), rotary_dim, 1 if interleaved else 0,
+                amplitude, addr(q_weight), addr(k_weight), eps, addr(q_out), addr(K), addr(V))
+
+
+def _paged_attention(where, cfg, n_req, T, q, K, V, block_table, lens, cu_new, out, lse, workspace):
+    n = T * cfg.n_q_heads
+    _paged_tensor(where, q, _paged_dtype(cfg), n * cfg.head_dim)
+    _paged_tensor(where, out, _paged_dtype(cfg), n * cfg.head_dim)
+    _paged_tensor(where, lse, torch.float32, n)
+    _paged_tensor(where, block_table, torch.int32, n_req * cfg.max_pages)
+    _paged_tensor(where, lens, torch.int32, n_req)
+    _paged_tensor(where, cu_new, torch.int32, n_req + 1)
+    _paged_pool(where, cfg, K, V)
+    return workspace.numel() * workspace.element_size() if torch.is_tensor(workspace) else 0
+
+
+def locret_paged_decode(cfg, n_req, q, K, V, block_table, lens, out, lse, workspace, stream=None, workspace_bytes=None) -> None:
+    where = "locret_paged_decode"
+    have = _paged_attention(where, cfg, n_req, n_req, q, K, V, block_table, lens, None, out, lse, workspace)
+    arrays = (q, K, V, block_table, lens, out, lse, workspace)
+    _paged_call(where, lib.locret_paged_decode, arrays, stream, C.byref(cfg), n_req, *map(_ptr, arrays),
+                have if workspace_bytes is None else workspace_bytes)
+
+
+def locret_paged_prefill(cfg, n_req, T, q, K, V, block_table, lens, cu_new, out, lse, workspace, stream=None, workspace_bytes=None) -> None:
+    where = "locret_paged_prefill"
+    have = _paged_attention(where, cfg, n_req, T, q, K, V, block_table, lens, cu_new, out, lse, workspace)
+    arrays = (q, K, V, block_table, lens, cu_new, out, lse, workspace)
+    _paged_call(where, lib.locret_paged_prefill, arrays, stream, C.byref(cfg), n_req, T, *map(_ptr, arrays),
+                have if workspace_bytes is None else workspace_bytes)
+
+
 # ---- convenience: config from a synth.Workload, a context that owns its workspace tensor -----------------
 def config_from_workload(w) -> locret_config:
     return locret_config(w.h, w.h_kv, w.d, w.B, w.b, w.d_R, w.rh_kv_expand,
@@ -349,3 +496,73 @@ class LocretLayer:
             self.close()
         except Exception:
             pass
+
+
+class PagedCache:
+    """Owns one layer's pool of pages, its bookkeeping and a workspace; methods forward to the C ABI (no arithmetic here).
+
+    A serving step: plan() gives the new tokens' places, append() brings their queries, keys and values there, decode() (one new token for each
+    of the first n_req requests) or prefill() (ragged chunks) attends.  `rope`: arguments of locret_rope_frequencies, None for no rotation."""
+
+    def __init__(self, cfg: locret_paged_config, device="cuda:0", rope=None, interleaved=False):
+        self.cfg, self.device = cfg, torch.device(device)
+        nbytes = locret_paged_workspace_bytes(cfg)
+        if nbytes == 0:
+            raise LocretError(LOCRET_EINVAL, "locret_paged_workspace_bytes")
+        self.tdtype = _paged_dtype(cfg)
+        ints = dict(dtype=torch.int32, device=self.device)
+        pool = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
+        self.K, self.V = torch.empty(pool, dtype=self.tdtype, device=self.device), torch.empty(pool, dtype=self.tdtype, device=self.device)
+        self.block_table = torch.zeros((cfg.max_reqs, cfg.max_pages), **ints)
+        self.lens = torch.zeros(cfg.max_reqs, **ints)
+        self.free_pages = torch.arange(cfg.n_pages - 1, -1, -1, **ints)
+        self.n_free = torch.full((1,), cfg.n_pages, **ints)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.rotary_dim, self.interleaved, self.amplitude, self.freq = 0, interleaved, 1.0, None
+        if rope is not None:
+            freq, self.amplitude = locret_rope_frequencies(**rope)
+            self.rotary_dim, self.freq = rope["rotary_dim"], torch.tensor(freq, dtype=torch.float64, device=self.device)
+
+    def plan(self, n_new, max_tokens: int):
+        """n_new int32 [n_req] on the device (-1: finished) -> (cu_new, slots, positions); lengths and pages are brought up to date."""
+        n, ints = n_new.shape[0], dict(dtype=torch.int32, device=self.device)
+        cu, slots, positions = torch.empty(n + 1, **ints), torch.empty(max_tokens, **ints), torch.empty(max_tokens, **ints)
+        locret_paged_plan(self.cfg, n, self.lens, n_new, self.lens, self.block_table, self.free_pages, self.n_free, self.n_free, max_tokens,
+                          cu, slots, positions)
+        return cu, slots, positions
+
+    def append(self, q, k, v, positions, slots, q_weight=None, k_weight=None, eps=1e-6):
+        """q [T][h][d], k, v [T][h_kv][d] -> the normed and rotated queries."""
+        out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+        locret_paged_append(self.cfg, q.shape[0], q, k, v, positions, slots, self.freq, self.rotary_dim, self.interleaved, self.amplitude,
+                            q_weight, k_weight, eps, out, self.K, self.V)
+        return out
+
+    def decode(self, q, want_lse=False):
+        out = torch.empty_like(q)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device) if want_lse else None
+        locret_paged_decode(self.cfg, q.shape[0], q, self.K, self.V, self.block_table, self.lens, out, lse, self.workspace)
+        return (out, lse) if want_lse else out
+
+    def prefill(self, q, cu_new, want_lse=False):
+        out = torch.zeros_like(q)
+        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=self.device) if want_lse else None
+        locret_paged_prefill(self.cfg, cu_new.shape[0] - 1, q.shape[0], q, self.K, self.V, self.block_table, self.lens, cu_new, out, lse,
+                             self.workspace)
+        return (out, lse) if want_lse else out
+
+    def adopt(self, layer: "LocretLayer", r: int) -> None:
+        """The retained cache of `layer` (its heads equally long, rows not packed) becomes the next units of request r, which generation
+        then continues: on an empty request, unit i sits at position i here as there."""
+        c, n = layer.cfg, layer.cache_len
+        if (c.n_kv_heads, c.head_dim, c.dtype) != (self.cfg.n_kv_heads, self.cfg.head_dim, self.cfg.dtype) or not 0 <= r < self.cfg.max_reqs:
+            raise LocretError(LOCRET_ESHAPE, "adopt")
+        if c.kv_bits or len(set(layer.cache_lens)) != 1 or layer.device != self.device:
+            raise LocretError(LOCRET_ESTATE, "adopt")
+        n_new = torch.zeros(r + 1, dtype=torch.int32, device=self.device)
+        n_new[r] = n
+        _, slots, positions = self.plan(n_new, n)
+        view = locret_cache_view(layer.ctx)
+        row, d = view["row_stride"], c.head_dim
+        locret_paged_append(self.cfg, n, None, view["K"], view["V"], positions, slots, self.freq, self.rotary_dim, self.interleaved, self.amplitude,
+                            None, None, 0.0, None, self.K, self.V, strides=[0, 0, d, row * d, d, row * d])

@@ -1,0 +1,78 @@
+// Internal interface of the paged entry points (paged_api.hip) to their kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace locret {
+
+struct PagedDims {
+  int h, h_kv, g, d;
+  int bf16;
+  int page_shift;       // log2 of the page size
+  int n_pages;
+  int max_pages;
+  int window, n_sink;   // window 0: none
+  float scale;
+};
+
+// One step's bookkeeping (locret_paged_plan).
+struct PagedPlan {
+  int n_req, max_tokens, page_shift, n_pages, max_pages;
+  const int32_t* lens;
+  const int32_t* n_new;
+  int32_t* lens_out;
+  int32_t* table;
+  int32_t* free_pages;
+  const int32_t* n_free;
+  int32_t* n_free_out;
+  int32_t* cu_new;
+  int32_t* slots;
+  int32_t* positions;
+};
+constexpr int PAGED_MAX_REQS = 4096;
+void launch_paged_plan(const PagedPlan& p, hipStream_t st);
+
+struct PagedRows {
+  int T;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;      // strides in elements
+  const int32_t* positions;
+  const int32_t* slots;
+  const double* freq;
+  int rot, interleaved;
+  float amplitude;
+  const float* q_weight;
+  const float* k_weight;
+  float eps;
+  void* q_out;
+  void* K;
+  void* V;
+};
+void launch_paged_append(const PagedDims& D, const PagedRows& a, hipStream_t st);
+
+// Attention of T query tokens over pages.  cu NULL: token t is the last unit of request t (T = n_req).
+struct PagedAttn {
+  int n_req, T;
+  const void* q;
+  const void* K;
+  const void* V;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* cu;
+  void* out;
+  float* lse;       // or NULL
+  void* ws;
+};
+void launch_paged_attn_simple(const PagedDims& D, const PagedAttn& a, hipStream_t st);
+
+// A length as the kernels take it.
+__device__ __forceinline__ int paged_len(const int32_t* lens, int r, int max_pages, int page_shift) {
+  return min(max(lens[r], 0), max_pages << page_shift);
+}
+
+// An entry of cu_new as the kernels take it.
+__device__ __forceinline__ int paged_cu(const int32_t* cu, int r, int T) { return min(max(cu[r], 0), T); }
+
+}  // namespace locret
