@@ -25,6 +25,7 @@ int validate(const locret_paged_config* c, PagedDims* D) {
   for (int s = 4; s <= 8; ++s) if (c->page_size == 1 << s) shift = s;
   if (!shift || c->max_reqs > PAGED_MAX_REQS) return LOCRET_ESHAPE;
   if (((int64_t)c->n_pages << shift) > INT32_MAX || ((int64_t)c->max_pages << shift) > INT32_MAX) return LOCRET_ESHAPE;
+  if (((int64_t)c->max_reqs * c->max_pages << shift) > (int64_t)1 << 37) return LOCRET_ESHAPE;     // units of work are counted in 32 bits
   D->h = c->n_q_heads;
   D->h_kv = c->n_kv_heads;
   D->g = D->h / D->h_kv;
@@ -39,7 +40,7 @@ int validate(const locret_paged_config* c, PagedDims* D) {
   return LOCRET_OK;
 }
 
-size_t workspace_bytes(const PagedDims&) { return 256; }
+size_t workspace_bytes(const PagedDims& D, int max_reqs) { return paged_decode_workspace(D, max_reqs); }
 
 int launched() { return hipGetLastError() == hipSuccess ? LOCRET_OK : LOCRET_EHIP; }
 
@@ -54,8 +55,9 @@ int attention(const locret_paged_config* cfg, const PagedAttn& a, size_t bytes, 
   if (misaligned(a.q) || misaligned(a.K) || misaligned(a.V) || misaligned(a.out) || misaligned(a.ws, 256) || misaligned(a.table, 4) ||
       misaligned(a.lens, 4) || misaligned(a.cu, 4) || misaligned(a.lse, 4))
     return LOCRET_EALIGN;
-  if (bytes < workspace_bytes(D)) return LOCRET_ENOMEM;
-  launch_paged_attn_simple(D, a, st);
+  if (bytes < workspace_bytes(D, cfg->max_reqs)) return LOCRET_ENOMEM;
+  if (prefill) launch_paged_attn_simple(D, a, st);
+  else launch_paged_decode(D, a, st);
   return launched();
 }
 
@@ -65,7 +67,7 @@ extern "C" {
 
 size_t locret_paged_workspace_bytes(const locret_paged_config* cfg) {
   PagedDims D;
-  return validate(cfg, &D) == LOCRET_OK ? workspace_bytes(D) : 0;
+  return validate(cfg, &D) == LOCRET_OK ? workspace_bytes(D, cfg->max_reqs) : 0;
 }
 
 int locret_paged_plan(const locret_paged_config* cfg, int32_t n_req, const int32_t* lens, const int32_t* n_new, int32_t* lens_out,

@@ -1,0 +1,475 @@
+// Attention of one new token per request over its pages (locret_paged_decode): split over the keys, joined by a second launch.
+//   s_j = scale q . k_j,  out = sum_j e^(s_j - M) v_j / L,  L = sum_j e^(s_j - M),  lse = M + ln L     over the visible keys j
+// Every key and value is read once for all query heads of its group, so HBM is the bound; both products run on the matrix cores with
+// the heads of a group (16 at a time) as one side of a 16 x 16 tile, so that the arithmetic stays far below that bound for any group.
+//
+// Work: an item is (request, KV head, 16 query heads), a unit 128 keys of an item (32 a wavefront).  Lengths are known on the device only, and
+// differ, so the units of all items are laid end to end and every workgroup takes the same number of them, as many workgroups
+// as the chip holds at once.  Each workgroup forms the sums of units over the requests by itself (at most 4096 numbers from L2, one scan) and
+// finds its first unit by bisection.  An item that one workgroup holds whole is written by it; of one that is cut, every
+// workgroup leaves maximum, sum and sum of values (two such pieces a workgroup at most), and the second launch, which has a workgroup
+// per request and head, joins them in the order of the keys.  Results depend on no order of execution.
+//
+// Tiles go from memory to registers in the layout of the operands (DecTile for bf16; PagedTileF32, whose products are exact to 32 bits):
+// S^T = K Q^T has keys as rows, in an order in which a lane's accumulators are the eight keys whose probabilities it gives to
+// O = P V.  The next keys are requested as soon as the logits are formed, the next values after their product, page numbers a unit
+// earlier.  Probabilities of bf16 layers become bf16 factors (half a step of 2^-8 each, as large as the rounding of the output, and
+// independent of each other, so less than that in a sum); maximum, sum and accumulators are 32-bit.  The maximum moves only when a logit
+// exceeds it by 8 binary orders.  What is not seen is taken out by selection: its logit before the maximum, its value before the product.
+#include "decode_tile.h"
+#include "paged.h"
+
+namespace locret {
+
+constexpr int PD_THREADS = 256, PD_NW = 4, PD_UNIT = 128, PD_HEADS = 16;
+constexpr float PD_RESCALE_LOG2 = 8.f;
+
+// Workgroups a CU: what registers allow without spilling.
+template <typename T, int D> struct PagedOcc { static constexpr int value = sizeof(T) == 2 ? (D >= 96 ? 3 : 4) : (D >= 96 ? 2 : 3); };
+static int paged_decode_workgroups(const PagedDims& D) { return 256 * (D.bf16 ? (D.d >= 96 ? 3 : 4) : (D.d >= 96 ? 2 : 3)); }
+
+// DecTile's operands from two places: rows 0..15 and 16..31 of the tile (pages of 16 units; the same place for larger ones).
+template <int D> struct PagedTileBf16 : DecTile<D> {
+  typedef DecTile<D> Base;
+  static constexpr int NQ = Base::NKS;
+  typedef bf16x8 q_t;
+  __device__ __forceinline__ void load_k(const bf16_t* lo, const bf16_t* hi) {
+    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
+    const bf16_t* base = (n >= 8 ? hi : lo) + (8 * (n >> 2) + (n & 3)) * D + kg * 8;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int ks = 0; ks < Base::NKS; ++ks) this->ka[b][ks] = *(const bf16x8*)(base + 4 * b * D + ks * 32);
+  }
+  __device__ __forceinline__ void load_v(const bf16_t* lo, const bf16_t* hi) {
+    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
+    const bf16_t* base = (kg >= 2 ? hi : lo) + 8 * kg * D + n * Base::NV;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) load_words<Base::NV / 2>(base + r * D, this->vw[r]);
+  }
+  __device__ __forceinline__ void clear_v(uint32_t seen) {          // bit r: the lane's key r
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int w = 0; w < Base::NV / 2; ++w) this->vw[r][w] = (seen >> r) & 1 ? this->vw[r][w] : 0u;
+  }
+  static __device__ __forceinline__ void load_q(const bf16_t* row, bool has, q_t (&qb)[NQ]) {
+    const int kg = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int ks = 0; ks < NQ; ++ks) qb[ks] = has ? *(const bf16x8*)(row + ks * 32 + kg * 8) : bf16x8{};
+  }
+  __device__ __forceinline__ void add(const float (&p)[8], dec_f32x4 (&o)[Base::NV]) const {
+    const uint4 pk = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
+    this->accumulate(__builtin_bit_cast(bf16x8, pk), o);
+  }
+};
+
+// The same for float: v_mfma_f32_16x16x4_f32.  Contraction step (ks, e) of S^T has dim 16 ks + 4 kg + e in lane group kg, so that a lane
+// reads 16 bytes; step r of a block's O = P V has key 4 kg + r there, which is where that key's probability is.
+template <int D> struct PagedTileF32 {
+  static constexpr int NQ = D / 16, NV = D / 16;
+  typedef float4 q_t;
+  float4 ka[2][NQ];
+  float vw[8][NV];
+  __device__ __forceinline__ void load_k(const float* lo, const float* hi) {
+    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
+    const float* base = (n >= 8 ? hi : lo) + (8 * (n >> 2) + (n & 3)) * D + kg * 4;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int ks = 0; ks < NQ; ++ks) ka[b][ks] = *(const float4*)(base + 4 * b * D + ks * 16);
+  }
+  __device__ __forceinline__ void load_v(const float* lo, const float* hi) {
+    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
+    const float* base = (kg >= 2 ? hi : lo) + 8 * kg * D + n * NV;
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int i = 0; i < NV; i += 2) *(float2*)&vw[r][i] = *(const float2*)(base + r * D + i);
+  }
+  __device__ __forceinline__ void clear_v(uint32_t seen) {
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) vw[r][i] = (seen >> r) & 1 ? vw[r][i] : 0.f;
+  }
+  static __device__ __forceinline__ void load_q(const float* row, bool has, q_t (&qb)[NQ]) {
+    const int kg = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int ks = 0; ks < NQ; ++ks) qb[ks] = has ? *(const float4*)(row + ks * 16 + kg * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void logits(const q_t (&qb)[NQ], dec_f32x4 (&s)[2]) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s[b] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < NQ; ++ks) {
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].x, qb[ks].x, s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].y, qb[ks].y, s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].z, qb[ks].z, s[b], 0, 0, 0);
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].w, qb[ks].w, s[b], 0, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void add(const float (&p)[8], dec_f32x4 (&o)[NV]) const {
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[r], vw[r][i], o[i], 0, 0, 0);
+  }
+};
+template <typename T, int D> struct PagedTileOf { typedef PagedTileBf16<D> type; };
+template <int D> struct PagedTileOf<float, D> { typedef PagedTileF32<D> type; };
+
+// The visible units of a request: its sinks, then from the first 32 keys with one in the window on.
+struct PagedSpan {
+  int n, w0, ns, wb, us, total;      // units in the cache, first key of the window, sinks in front of it, its first tile, units of either
+};
+__device__ __forceinline__ PagedSpan paged_span(int n, int window, int n_sink) {
+  PagedSpan s;
+  s.n = n;
+  s.w0 = window ? max(0, n - window) : 0;
+  s.ns = min(n_sink, s.w0);
+  s.wb = s.w0 & ~31;
+  s.us = (s.ns + PD_UNIT - 1) / PD_UNIT;
+  s.total = s.us + (n - s.wb + PD_UNIT - 1) / PD_UNIT;
+  return s;
+}
+
+// Where a piece lies in the workspace.
+struct PagedPieces {
+  int32_t* first;     // [n_req + 1] units of one head before each request (their sum fits by the configuration's limits)
+  float2* ml;         // [2 workgroups][16] maximum (log2) and sum
+  float* o;           // [2 workgroups][16][d]
+};
+__host__ __device__ inline PagedPieces paged_pieces(void* ws, int n_req, int n_wg) {
+  PagedPieces p;
+  p.first = (int32_t*)ws;
+  p.ml = (float2*)((char*)ws + (((size_t)(n_req + 1) * 4 + 255) & ~(size_t)255));
+  p.o = (float*)(p.ml + (size_t)2 * n_wg * PD_HEADS);
+  return p;
+}
+size_t paged_decode_workspace(const PagedDims& D, int max_reqs) {
+  const int n_wg = paged_decode_workgroups(D), rows = D.g < PD_HEADS ? D.g : PD_HEADS;
+  return (size_t)((char*)paged_pieces(nullptr, max_reqs, n_wg).o - (char*)nullptr) + (size_t)2 * n_wg * rows * D.d * sizeof(float);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_decode_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm,
+                                                                                           int passes, int ipt) {
+  typedef typename PagedTileOf<T, D>::type Tile;
+  constexpr int NV = D / 16;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ float2 wml[PD_NW][PD_HEADS];
+  __shared__ int64_t scan[PD_NW];
+  float* sets = (float*)smem;                              // [wavefront][rows][D]
+  const int rows_max = min(Dm.g, PD_HEADS);
+  int32_t* first = (int32_t*)(smem + (size_t)PD_NW * rows_max * D * sizeof(float));
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, kg = lane >> 4;
+  const PagedPieces pc = paged_pieces(a.ws, a.n_req, gridDim.x);
+
+  // units of one head before every request
+  int64_t mine = 0, total;
+  for (int u = 0; u < ipt; ++u) {
+    const int r = tid * ipt + u;
+    if (r < a.n_req) {
+      const int t = paged_span(paged_len(a.lens, r, Dm.max_pages, Dm.page_shift), Dm.window, Dm.n_sink).total;
+      first[r + 1] = t;
+      mine += t;
+    }
+  }
+  int64_t before = block_exclusive(mine, scan, total);
+  for (int u = 0; u < ipt; ++u) {
+    const int r = tid * ipt + u;
+    if (r < a.n_req) {
+      before += first[r + 1];
+      first[r + 1] = (int)before;
+      if (blockIdx.x == 0) pc.first[r + 1] = (int)before;
+    }
+  }
+  if (tid == 0) {
+    first[0] = 0;
+    if (blockIdx.x == 0) pc.first[0] = 0;
+  }
+  __syncthreads();
+  const int items = Dm.h_kv * passes;
+  const int64_t all = total * items, per = (all + gridDim.x - 1) / gridDim.x;
+  int64_t u = per * blockIdx.x;
+  const int64_t u_end = min(all, u + per);
+  if (u >= u_end) return;
+  int r = 0, item, tile;
+  {
+    int lo = 0, hi = a.n_req - 1;                          // the last request that begins at or before u
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((int64_t)first[mid] * items <= u) lo = mid; else hi = mid - 1;
+    }
+    r = __builtin_amdgcn_readfirstlane(lo);
+    const int64_t in = u - (int64_t)first[r] * items, t = first[r + 1] - first[r];
+    item = __builtin_amdgcn_readfirstlane((int)(in / t));
+    tile = __builtin_amdgcn_readfirstlane((int)(in % t));
+  }
+  const float c = Dm.scale * 1.4426950408889634f;
+  const int shift = Dm.page_shift, page = 1 << shift;
+  bool begun = false;                                      // this workgroup has left a piece already: the next one goes to the second place
+
+  while (u < u_end) {
+    const PagedSpan sp = paged_span(paged_len(a.lens, r, Dm.max_pages, shift), Dm.window, Dm.n_sink);
+    const int m = item / passes, hp = item % passes;
+    const int j0 = m * Dm.g + hp * PD_HEADS, ng = min(PD_HEADS, Dm.g - hp * PD_HEADS);
+    const int t_end = (int)min((int64_t)sp.total, tile + (u_end - u));
+    const int32_t* row = table + (int64_t)r * Dm.max_pages;
+    const T* Kp = (const T*)a.K + (int64_t)m * page * D;
+    const T* Vp = (const T*)a.V + (int64_t)m * page * D;
+    const int64_t page_stride = (int64_t)Dm.h_kv * page * D;
+
+    // tile t of this wavefront: its keys kb .. kb + 31 of [lo, hi) and its two page numbers
+    struct Place { int kb, lo, hi, id0, id1; };
+    auto place = [&](int t) __attribute__((always_inline)) {
+      Place p;
+      const bool sink = t < sp.us;
+      p.kb = (sink ? t * PD_UNIT : sp.wb + (t - sp.us) * PD_UNIT) + wave * 32;
+      p.lo = sink ? 0 : sp.w0;
+      p.hi = sink ? sp.ns : sp.n;
+      p.id0 = p.id1 = -1;
+      if (p.kb < p.hi) {
+        p.id0 = row[p.kb >> shift];
+        p.id1 = shift == 4 ? (p.kb + 16 < p.hi ? row[(p.kb >> 4) + 1] : -1) : p.id0;
+      }
+      return p;
+    };
+    auto address = [&](const T* base, const Place& p, const T*& lo, const T*& hi) __attribute__((always_inline)) {
+      // (a number that is not the pool's: page 0, whose rows are masked then)
+      const int i0 = (unsigned)p.id0 < (unsigned)Dm.n_pages ? p.id0 : 0, i1 = (unsigned)p.id1 < (unsigned)Dm.n_pages ? p.id1 : 0;
+      lo = base + i0 * page_stride + (p.kb & (page - 1)) * D;
+      hi = shift == 4 ? base + i1 * page_stride - 16 * D : lo;
+    };
+
+    typename Tile::q_t qb[Tile::NQ];
+    Tile::load_q((const T*)a.q + ((int64_t)r * Dm.h + j0 + min(n, ng - 1)) * D, n < ng, qb);
+    Tile tl;
+    Place p = place(tile);
+    if (p.kb < p.hi) {
+      const T *lo, *hi;
+      address(Kp, p, lo, hi);
+      tl.load_k(lo, hi);
+      address(Vp, p, lo, hi);
+      tl.load_v(lo, hi);
+    }
+    dec_f32x4 o[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) o[i] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
+    float mrun = -INFINITY, lrun = 0.f;
+    Place nx = place(min(tile + 1, t_end - 1));
+    for (int t = tile; t < t_end; ++t) {
+      const Place nn = place(min(t + 2, t_end - 1));
+      const bool work = p.kb < p.hi && p.kb + 32 > p.lo, more = t + 1 < t_end && nx.kb < nx.hi;
+      dec_f32x4 s[2];
+      float pr[8];
+      if (p.kb < p.hi) tl.logits(qb, s);
+      const T *klo, *khi;
+      if (more) {
+        address(Kp, nx, klo, khi);
+        tl.load_k(klo, khi);
+      }
+      if (work) {
+        uint32_t seen = 0xffu;
+        if (p.kb < p.lo || p.kb + 32 > p.hi || (unsigned)p.id0 >= (unsigned)Dm.n_pages || (unsigned)p.id1 >= (unsigned)Dm.n_pages) {
+          seen = 0;
+          const int id = kg >= 2 ? p.id1 : p.id0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int key = p.kb + 8 * kg + j;
+            seen |= (key >= p.lo && key < p.hi && (unsigned)id < (unsigned)Dm.n_pages) ? 1u << j : 0u;
+          }
+          tl.clear_v(seen);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s[j >> 2][j & 3] = (seen >> j) & 1 ? s[j >> 2][j & 3] : -INFINITY;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, s[j >> 2][j & 3]);
+        mx *= c;
+        if (__any((mx - mrun) > PD_RESCALE_LOG2)) {        // also true from -inf to a number
+          mx = max_across_quarters(mx);                    // the four lanes of a column move together
+          const bool up = (mx - mrun) > PD_RESCALE_LOG2;
+          const float alpha = up ? __builtin_amdgcn_exp2f(mrun - mx) : 1.f;
+          if (up) mrun = mx;
+          lrun *= alpha;
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr) {
+            const float ar = __shfl(alpha, 4 * kg + rr, 64);      // accumulator row 4 kg + rr is that head
+#pragma unroll
+            for (int i = 0; i < NV; ++i) o[i][rr] *= ar;
+          }
+        }
+        const float ref = mrun == -INFINITY ? 0.f : mrun;  // (nothing seen yet, or every logit so far is -inf)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          pr[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], c, -ref));
+          lrun += pr[j];
+        }
+        tl.add(pr, o);
+      }
+      if (more) {
+        address(Vp, nx, klo, khi);
+        tl.load_v(klo, khi);
+      }
+      p = nx;
+      nx = nn;
+    }
+    lrun = sum_across_quarters(lrun);
+    // ---- the wavefronts' results together ------------------------------------------------------------------------------
+#pragma unroll
+    for (int rr = 0; rr < 4; ++rr) {
+      const int head = 4 * kg + rr;
+      if (head < ng)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) sets[(wave * rows_max + head) * D + n * NV + i] = o[i][rr];
+    }
+    if (lane < PD_HEADS) wml[wave][lane] = make_float2(mrun, lrun);
+    __syncthreads();
+    const bool whole = tile == 0 && t_end == sp.total;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (begun ? 1 : 0);
+    for (int idx = tid; idx < ng * (D / 4); idx += PD_THREADS) {
+      const int head = idx / (D / 4), e = idx % (D / 4) * 4;
+      float M = -INFINITY, L = 0.f;
+#pragma unroll
+      for (int w = 0; w < PD_NW; ++w) M = fmaxf(M, wml[w][head].x);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < PD_NW; ++w) {
+        const float2 ml = wml[w][head];
+        // a wavefront whose maximum is -inf has seen nothing, or only logits of -inf or NaN: its sum says which
+        const float wt = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - M);
+        const float4 y = *(const float4*)&sets[(w * rows_max + head) * D + e];
+        L = fmaf(wt, ml.y, L);
+        if (wt != 0.f) { x.x = fmaf(wt, y.x, x.x); x.y = fmaf(wt, y.y, x.y); x.z = fmaf(wt, y.z, x.z); x.w = fmaf(wt, y.w, x.w); }
+      }
+      if (whole) {
+        const int64_t at = (int64_t)r * Dm.h + j0 + head;
+        const bool none = M == -INFINITY && L == 0.f;
+        const float inv = none ? 0.f : 1.f / L;
+        T* dst = (T*)a.out + at * D + e;
+        Elem<T>::st(dst, none ? 0.f : x.x * inv);
+        Elem<T>::st(dst + 1, none ? 0.f : x.y * inv);
+        Elem<T>::st(dst + 2, none ? 0.f : x.z * inv);
+        Elem<T>::st(dst + 3, none ? 0.f : x.w * inv);
+        if (a.lse && e == 0) a.lse[at] = none ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+      } else {
+        *(float4*)&pc.o[(slot * rows_max + head) * D + e] = x;
+        if (e == 0) pc.ml[slot * PD_HEADS + head] = make_float2(M, L);
+      }
+    }
+    begun = begun || !whole;
+    __syncthreads();
+    u += t_end - tile;
+    tile = 0;
+    if (++item == items) {
+      item = 0;
+      do ++r; while (u < u_end && first[r + 1] == first[r]);
+    }
+  }
+}
+
+// Joins the pieces of the items that were cut, and answers for requests that see nothing.  One workgroup per (head, request); its threads
+// are dims / 4 x groups of pieces, each of which goes over every NP-th piece with a running maximum.
+template <typename T, int D>
+__global__ __launch_bounds__(PD_THREADS) void paged_decode_join_kernel(PagedAttn a, PagedDims Dm, int passes, int n_wg) {
+  constexpr int E = D / 4, NP = PD_THREADS / E;
+  __shared__ float4 so[NP][E];
+  __shared__ float2 sml[NP];
+  const int j = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, e = tid % E, g = tid / E;
+  const PagedPieces pc = paged_pieces(a.ws, a.n_req, n_wg);
+  const int f0 = pc.first[r], t = pc.first[r + 1] - f0;
+  const int64_t at = (int64_t)r * Dm.h + j;
+  if (t == 0) {
+    if (g == 0)
+      for (int i = 0; i < 4; ++i) Elem<T>::st((T*)a.out + at * D + e * 4 + i, 0.f);
+    if (a.lse && tid == 0) a.lse[at] = -INFINITY;
+    return;
+  }
+  const int items = Dm.h_kv * passes, in = j % Dm.g, item = j / Dm.g * passes + in / PD_HEADS, head = in % PD_HEADS, rows_max = min(Dm.g, PD_HEADS);
+  const int64_t per = ((int64_t)pc.first[a.n_req] * items + n_wg - 1) / n_wg, u0 = (int64_t)f0 * items + (int64_t)item * t, u1 = u0 + t;
+  const int w0 = (int)(u0 / per), w1 = (int)((u1 - 1) / per);
+  if (w0 == w1) return;
+  // the first workgroup's piece: its second place if it had left one before, that is if its first item was cut at its start and ended there
+  const int64_t b0 = per * w0;
+  bool second = false;
+  if (b0 < u0) {
+    // the item that unit b0 belongs to began before b0?
+    int lo = 0, hi = r;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((int64_t)pc.first[mid] * items <= b0) lo = mid; else hi = mid - 1;
+    }
+    second = (b0 - (int64_t)pc.first[lo] * items) % (pc.first[lo + 1] - pc.first[lo]) != 0;
+  }
+  float M = -INFINITY, L = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (g < NP) {
+    for (int w = w0 + g; w <= w1; w += NP) {
+      const int64_t slot = 2 * (int64_t)w + (w == w0 && second ? 1 : 0);
+      const float2 ml = pc.ml[slot * PD_HEADS + head];
+      const float4 y = *(const float4*)&pc.o[(slot * rows_max + head) * D + e * 4];
+      if (ml.y == 0.f) continue;                           // saw nothing (a sum of NaN is not 0)
+      const float Mn = fmaxf(M, ml.x), ref = Mn == -INFINITY ? 0.f : Mn;
+      const float wa = M == -INFINITY ? (L == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(M - ref), wb = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
+      L = (wa == 0.f ? 0.f : wa * L) + wb * ml.y;
+      x.x = (wa == 0.f ? 0.f : wa * x.x) + wb * y.x;
+      x.y = (wa == 0.f ? 0.f : wa * x.y) + wb * y.y;
+      x.z = (wa == 0.f ? 0.f : wa * x.z) + wb * y.z;
+      x.w = (wa == 0.f ? 0.f : wa * x.w) + wb * y.w;
+      M = Mn;
+    }
+    so[g][e] = x;
+    if (e == 0) sml[g] = make_float2(M, L);
+  }
+  __syncthreads();
+  if (tid >= E) return;
+  M = -INFINITY;
+  L = 0.f;
+#pragma unroll
+  for (int p = 0; p < NP; ++p) M = fmaxf(M, sml[p].x);
+  x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const float2 ml = sml[p];
+    if (ml.y == 0.f) continue;
+    const float wt = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float4 y = so[p][e];
+    L += wt * ml.y;
+    x.x += wt * y.x; x.y += wt * y.y; x.z += wt * y.z; x.w += wt * y.w;
+  }
+  const bool none = M == -INFINITY && L == 0.f;
+  const float inv = none ? 0.f : 1.f / L;
+  T* dst = (T*)a.out + at * D + e * 4;
+  Elem<T>::st(dst, none ? 0.f : x.x * inv);
+  Elem<T>::st(dst + 1, none ? 0.f : x.y * inv);
+  Elem<T>::st(dst + 2, none ? 0.f : x.z * inv);
+  Elem<T>::st(dst + 3, none ? 0.f : x.w * inv);
+  if (a.lse && tid == 0) a.lse[at] = none ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.6931471805599453f;
+}
+
+template <typename T, int D>
+static void decode_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t st) {
+  const int n_wg = paged_decode_workgroups(Dm), passes = (Dm.g + PD_HEADS - 1) / PD_HEADS;
+  const int rows = Dm.g < PD_HEADS ? Dm.g : PD_HEADS, ipt = (a.n_req + PD_THREADS - 1) / PD_THREADS;
+  const size_t lds = (size_t)PD_NW * rows * D * sizeof(float) + (size_t)(a.n_req + 1) * sizeof(int32_t);
+  paged_decode_kernel<T, D><<<(unsigned)n_wg, PD_THREADS, lds, st>>>(a, a.table, Dm, passes, ipt);
+  paged_decode_join_kernel<T, D><<<dim3((unsigned)Dm.h, (unsigned)a.n_req), PD_THREADS, 0, st>>>(a, Dm, passes, n_wg);
+}
+
+void launch_paged_decode(const PagedDims& D, const PagedAttn& a, hipStream_t st) {
+#define LOCRET_DECODE(T)                        \
+  switch (D.d) {                                \
+    case 32: decode_d<T, 32>(D, a, st); break;  \
+    case 64: decode_d<T, 64>(D, a, st); break;  \
+    case 96: decode_d<T, 96>(D, a, st); break;  \
+    default: decode_d<T, 128>(D, a, st); break; \
+  }
+  if (D.bf16) { LOCRET_DECODE(bf16_t) } else { LOCRET_DECODE(float) }
+#undef LOCRET_DECODE
+}
+
+}  // namespace locret

@@ -24,33 +24,6 @@ struct PlanSmem {
   int64_t part[3][PLAN_MAX_THREADS / 64];
 };
 
-__device__ __forceinline__ int64_t shfl_up64(int64_t x, int by) {
-  const int lo = __shfl_up((int)(uint32_t)x, by, 64), hi = __shfl_up((int)(x >> 32), by, 64);
-  return (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
-}
-
-// Exclusive sums of x over the workgroup's threads; `total` gets the sum of all.  part: one entry a wavefront, not in use by others
-// until the next barrier but one.
-__device__ __forceinline__ int64_t block_exclusive(int64_t x, int64_t* part, int64_t& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  int64_t s = x;
-#pragma unroll
-  for (int by = 1; by < 64; by <<= 1) {
-    const int64_t y = shfl_up64(s, by);
-    if (lane >= by) s += y;
-  }
-  if (lane == 63) part[wave] = s;
-  __syncthreads();
-  int64_t before = 0;
-  total = 0;
-  for (int w = 0; w < nw; ++w) {
-    const int64_t y = part[w];
-    if (w < wave) before += y;
-    total += y;
-  }
-  return before + s - x;
-}
-
 __device__ __forceinline__ int pages_of(int units, int shift) { return (int)(((int64_t)units + (1 << shift) - 1) >> shift); }
 
 // Table entries of requests r0, r0 + r_step, ... (a wavefront each) and slots of the tokens [t0, t1), from the sums in LDS.
