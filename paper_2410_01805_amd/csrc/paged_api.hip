@@ -40,7 +40,10 @@ int validate(const locret_paged_config* c, PagedDims* D) {
   return LOCRET_OK;
 }
 
-size_t workspace_bytes(const PagedDims& D, int max_reqs) { return paged_decode_workspace(D, max_reqs); }
+size_t workspace_bytes(const PagedDims& D, int max_reqs) {
+  const size_t a = paged_decode_workspace(D, max_reqs), b = paged_prefill_workspace(D);
+  return a > b ? a : b;
+}
 
 int launched() { return hipGetLastError() == hipSuccess ? LOCRET_OK : LOCRET_EHIP; }
 
@@ -49,14 +52,15 @@ int attention(const locret_paged_config* cfg, const PagedAttn& a, size_t bytes, 
   const int rc = validate(cfg, &D);
   if (rc != LOCRET_OK) return rc;
   if (a.n_req < 0 || a.T < 0) return LOCRET_EINVAL;
-  if (a.n_req > cfg->max_reqs) return LOCRET_ESHAPE;
+  if (a.n_req > cfg->max_reqs || (int64_t)a.T * D.h > (int64_t)1 << 37) return LOCRET_ESHAPE;      // (launches are counted in 32 bits)
   if (a.n_req == 0 || a.T == 0) return LOCRET_OK;
   if (!a.q || !a.K || !a.V || !a.table || !a.lens || (prefill && !a.cu) || !a.out || !a.ws) return LOCRET_EINVAL;
   if (misaligned(a.q) || misaligned(a.K) || misaligned(a.V) || misaligned(a.out) || misaligned(a.ws, 256) || misaligned(a.table, 4) ||
       misaligned(a.lens, 4) || misaligned(a.cu, 4) || misaligned(a.lse, 4))
     return LOCRET_EALIGN;
   if (bytes < workspace_bytes(D, cfg->max_reqs)) return LOCRET_ENOMEM;
-  if (prefill) launch_paged_attn_simple(D, a, st);
+  if (prefill && D.bf16) launch_paged_prefill(D, a, st);
+  else if (prefill) launch_paged_attn_simple(D, a, st);
   else launch_paged_decode(D, a, st);
   return launched();
 }

@@ -1,0 +1,568 @@
+// Causal attention of a ragged batch of chunks over pages (locret_paged_prefill), bf16, on the matrix cores.
+//   s_tj = scale q_t . k_j over the visible keys j of query t,  out_t = sum_j e^(s_tj - M_t) v_j / L_t,  lse_t = M_t + ln L_t
+// Bound by the matrix cores: 4 d operations for each (query, key) pair against 4 d bytes for each key of 256 query rows.
+//
+// A workgroup takes 256 rows (token, query head of one KV head), 256 / g whole tokens of one request, so that short chunks
+// fill it for any group size, and goes over the keys that any of them sees: first the sinks, then from the window of its first token to
+// its last token.  Its 8 wavefronts have 32 rows each.  Products are transposed, v_mfma_f32_32x32x16_bf16: S^T = K Q^T (A = 32 keys from
+// LDS, B = the rows' queries in registers), O^T += V^T P^T (A = V^T by the transposing LDS read, B = P^T as the S accumulators hold it: 16
+// keys of one row a lane, so that sums are per lane).  Wavefronts 0..3 and 4..7, two of which share a SIMD, are held one S block apart by
+// two barriers a tile, X and Y, so that the matrix pipe has S and PV of one half while the other is at its softmax:
+//
+//      X(t) | A: S(t)                     | Y(t) | A: softmax, PV, first K fragments of t+1
+//           | B: loads of t+3, K fragments |      | B: S(t), softmax, PV
+//
+// Tiles (64 keys of 128 or 96 dims, 128 of 64 or 32) come from the pages to a ring of 4 stages in LDS without passing through registers: a
+// load instruction of a wavefront covers 1 KB of LDS, which is 4 or 8 keys and lies inside 16 keys that start at a multiple of 16, so it
+// lies inside one page of any size, and has a descriptor of its own: base = those keys in the page, length = how many of them are
+// there.  What is behind the last key, on no page, or padding of a row arrives as zeros.  LDS rows have 256 bytes (keys of 64 or 32 dims lie two
+// in a row); position c' of row r holds the 16-byte chunk c' ^ f(r), with f chosen so that neither the fragment reads of K nor the
+// transposing ones of V meet in a bank: f = r mod 16 for K; 4 (r mod 4), or 4 (r mod 2) with two keys in a row, for V.
+// At X(t) tiles t and t+1 are in LDS, and every wavefront is done with t-1, whose stage the loads of t+3 overwrite.
+//
+// Softmax: logits stay unscaled in the accumulators and become exponents by one multiply-add (queries scaled before the product would have
+// to be rounded again, which costs the outputs twice the error).  The running maximum of a row is that of the first tile in which it sees
+// a key, and raised when the row's sum over a tile reaches 2^30.  Probabilities become bf16 factors, half a step of 2^-8 each; sums, maxima
+// and accumulators are 32-bit.
+// Tiles that some row of a wavefront does not see whole are masked before the maximum.  A masked probability is 0, but 0 times a value that is
+// not finite is not, so such a tile's values are looked through first, and if one is not finite the tile's product is
+// formed key by key for the rows that see it.
+//
+// Few rows: where the items (tokens tile, KV head) are at most half as many as the CUs, each one's keys are cut into parts,
+// workgroups of their own, which leave maximum, sum and accumulators; a second launch joins them.
+#include "attn_common.h"
+#include "paged.h"
+
+namespace locret {
+
+typedef __attribute__((address_space(3))) void* pf_lds_ptr;
+typedef __attribute__((address_space(3))) unsigned char* pf_lds_u8;
+typedef short pf_s16x4 __attribute__((ext_vector_type(4)));
+typedef short pf_s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int PF_NW = 8, PF_THREADS = PF_NW * 64, PF_ROWS = PF_NW * 32;
+constexpr int PF_TILE_B = 64 * 256, PF_STAGE_B = 2 * PF_TILE_B;
+constexpr int PF_KPRE = 4;                     // K fragments fetched ahead of the S block
+constexpr int PF_CUS = 256, PF_MAX_PARTS = 16, PF_MAX_SLOTS = 256;
+constexpr int PF_MIN_PART = 4;                 // key tiles of a part at least: less does not pay for a part's prologue and joining
+
+// What a workgroup works on.
+struct PfItem {
+  int r, m, t0, n_tok;      // request, KV head, first token (in the packed order) and tokens
+  int p0;                   // position of the first token
+};
+
+#define LOCRET_PF_TR(dst, addr, off) asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "i"(off) : "memory")
+#define LOCRET_PF_WAIT(a, b, n) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "i"(n))
+
+// Finds item x = (token tile, KV head): the token tiles of all requests in their order, a request's last tile first (it sees the most keys).
+// first: LDS, n_req + 1 ints, free again after the next barrier.  False: there is no such tile.  All results are the same in the whole workgroup.
+__device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm, int x, int32_t* first, PfItem& it) {
+  __shared__ int64_t scan[PF_NW];
+  const int tid = threadIdx.x, tw = PF_ROWS / Dm.g, ipt = (a.n_req + PF_THREADS - 1) / PF_THREADS;
+  int64_t mine = 0, total;
+  for (int u = 0; u < ipt; ++u) {
+    const int r = tid * ipt + u;
+    if (r < a.n_req) {
+      const int c0 = paged_cu(a.cu, r, a.T), n = max(paged_cu(a.cu, r + 1, a.T) - c0, 0);
+      first[r + 1] = (n + tw - 1) / tw;
+      mine += first[r + 1];
+    }
+  }
+  int64_t before = block_exclusive(mine, scan, total);
+  for (int u = 0; u < ipt; ++u) {
+    const int r = tid * ipt + u;
+    if (r < a.n_req) {
+      before += first[r + 1];
+      first[r + 1] = (int)before;
+    }
+  }
+  if (tid == 0) first[0] = 0;
+  __syncthreads();
+  // every eighth workgroup is on the same XCD: a KV head's items on one of them, where they find its pages in one L2
+  int tile;
+  if (Dm.h_kv % 8 == 0) {
+    const int per = Dm.h_kv / 8;
+    it.m = (x & 7) * per + (x >> 3) % per;
+  } else {
+    it.m = x % Dm.h_kv;
+  }
+  tile = x / Dm.h_kv;
+  if (tile >= total) return false;
+  int lo = 0, hi = a.n_req - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= tile) lo = mid; else hi = mid - 1;
+  }
+  const int tt = first[lo + 1] - 1 - tile;
+  const int c0 = paged_cu(a.cu, lo, a.T), n = paged_cu(a.cu, lo + 1, a.T) - c0;
+  it.r = __builtin_amdgcn_readfirstlane(lo);
+  it.t0 = __builtin_amdgcn_readfirstlane(c0 + tt * tw);
+  it.n_tok = __builtin_amdgcn_readfirstlane(min(tw, n - tt * tw));
+  it.p0 = __builtin_amdgcn_readfirstlane(paged_len(a.lens, lo, Dm.max_pages, Dm.page_shift) - n + tt * tw);
+  it.m = __builtin_amdgcn_readfirstlane(it.m);
+  return true;
+}
+
+// The keys of an item: sink tiles from 0, then window tiles from wb, up to n_keys.
+struct PfKeys {
+  int n_keys, w_lo, ns, wb, ns_t, n_tiles;
+};
+__device__ __forceinline__ PfKeys pf_keys(const PfItem& it, const PagedDims& Dm, int KT) {
+  PfKeys k;
+  k.n_keys = max(it.p0 + it.n_tok, 0);                    // (positions below 0 see nothing)
+  k.w_lo = Dm.window ? max(0, it.p0 - Dm.window + 1) : 0;
+  k.ns = min(Dm.n_sink, k.w_lo);
+  k.wb = k.w_lo & ~15;
+  k.ns_t = (k.ns + KT - 1) / KT;
+  k.n_tiles = k.ns_t + (max(k.n_keys - k.wb, 0) + KT - 1) / KT;
+  return k;
+}
+// Parts of an item and the tiles of each.
+__device__ __forceinline__ int pf_part_len(int n_tiles, int k) { return max((n_tiles + k - 1) / k, PF_MIN_PART); }
+
+__host__ __device__ constexpr int pf_tile_keys(int d) { return d <= 64 ? 128 : 64; }
+
+template <int D>
+__global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm, int n_items,
+                                                                     int parts, float* __restrict__ part) {
+  constexpr int KH = D <= 64 ? 2 : 1;                      // keys of an LDS row
+  constexpr int KT = 64 * KH, NKB = KT / 32;               // keys and 32-key blocks of a tile
+  constexpr int NKS = D / 16, NDB = D / 32;                // contraction steps of S, 32-dim blocks of O^T
+  constexpr int NKF = NKB * NKS, NVF = KT / 16 * NDB;      // K and V^T fragments of a tile
+  constexpr int VPRE = KH == 2 ? 2 : 4;                    // V^T fragments in flight ahead of their MFMA
+  constexpr int KC_B = 4096 / KH, KC_H = 2048 / KH;        // bytes of 16 keys and of 8 keys in LDS
+  constexpr int YTAIL = D == 128 ? 4 : 1;                  // MFMAs of A's S block behind barrier Y
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * PF_STAGE_B];
+
+  PfItem it;
+  const int layer = blockIdx.x / n_items;
+  if (!pf_item(a, Dm, blockIdx.x - layer * n_items, (int32_t*)ring, it)) return;
+  const PfKeys ks_ = pf_keys(it, Dm, KT);
+  int t_lo = 0, t_hi = ks_.n_tiles;
+  bool cut = false;
+  if (parts > 1) {
+    const int len = pf_part_len(ks_.n_tiles, parts);
+    cut = ks_.n_tiles > len;
+    t_lo = layer * len;
+    t_hi = min(t_hi, t_lo + len);
+    if (layer > 0 && t_lo >= ks_.n_tiles) return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, n32 = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = Dm.g, shift = Dm.page_shift, page = 1 << shift;
+  const int rows = it.n_tok * g;
+  const int32_t* trow = table + (int64_t)it.r * Dm.max_pages;
+
+  // pages that are not the pool's, among those of the item's keys
+  bool odd_pages;
+  {
+    int odd = 0;
+    const int s_end = (ks_.ns + page - 1) >> shift, e0 = ks_.wb >> shift, e1 = (ks_.n_keys + page - 1) >> shift;
+    for (int i = tid; i < s_end; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
+    for (int i = e0 + tid; i < e1; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
+    odd_pages = __syncthreads_or(odd);                     // (also: `ring` no longer holds the sums of pf_item)
+  }
+
+  // this lane's row, and the first and last position of the wavefront's
+  const int row = min(wave * 32 + n32, rows - 1), tok = row / g;
+  const int64_t at = (int64_t)(it.t0 + tok) * Dm.h + it.m * g + (row - tok * g);
+  const int pos = it.p0 + tok;
+  const int pw0 = it.p0 + min(wave * 32, rows - 1) / g, pw1 = it.p0 + min(wave * 32 + 31, rows - 1) / g;
+  const bool has_rows = wave * 32 < rows;
+
+  bf16x8 qf[NKS];
+  {
+    const bf16_t* qp = (const bf16_t*)a.q + at * D + hi * 8;
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) qf[s] = *(const bf16x8*)(qp + s * 16);
+  }
+  f32x16 oacc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+  const float c = Dm.scale * 1.4426950408889634f;
+  float m_run = 0.f, l_run = 0.f;              // of the lane's row, in log2 units; the sum over this lane's keys
+  bool unset = true;                           // the row has seen no key yet
+
+  // ---- tiles -----------------------------------------------------------------------------------------------------------
+  auto tile_key = [&](int t) __attribute__((always_inline)) { return t < ks_.ns_t ? t * KT : ks_.wb + (t - ks_.ns_t) * KT; };
+  const int w4 = wave & 3, l_row = lane >> 4, l_pos = lane & 15;
+  constexpr int NCH = D / 8, SLOT = 16 / KH, KPI = 4 * KH;       // chunks of a key in memory and in LDS; keys of a load instruction
+  constexpr int OUTSIDE = 0x7ffff000;                            // an offset no descriptor reaches: the load brings zeros
+  auto offset = [&](int ch) { return ch % SLOT < NCH ? (l_row * KH + ch / SLOT) * (D * 2) + ch % SLOT * 16 : OUTSIDE; };
+  const int k_vo = offset(l_pos ^ l_row ^ (w4 << 2)), v_vo = offset(l_pos ^ ((KH == 1 ? l_row : l_row & 1) << 2));
+  const int64_t page_stride = (int64_t)Dm.h_kv * page * D;
+  const bf16_t* Kp = (const bf16_t*)a.K + (int64_t)it.m * page * D;
+  const bf16_t* Vp = (const bf16_t*)a.V + (int64_t)it.m * page * D;
+  int ids[4];                                                    // page numbers of the tile that is loaded next
+  auto load_ids = [&](int t) __attribute__((always_inline)) {
+    const int tu = __builtin_amdgcn_readfirstlane(t);
+    const int kb = tile_key(tu), end = tu >= t_hi ? 0 : tu < ks_.ns_t ? ks_.ns : ks_.n_keys;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int key = kb + (w4 + u * 4) * KPI;
+      ids[u] = -1;
+      if (key < end) ids[u] = trow[key >> shift];
+    }
+  };
+  auto issue = [&](int t, int stage) __attribute__((always_inline)) {
+    const int tu = __builtin_amdgcn_readfirstlane(t);
+    const int kb = tile_key(tu), end = tu >= t_hi ? 0 : tu < ks_.ns_t ? ks_.ns : ks_.n_keys;
+    unsigned char* sb = ring + stage * PF_STAGE_B;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = w4 + u * 4, key = kb + i * KPI;
+      const int id = __builtin_amdgcn_readfirstlane(ids[u]);
+      const bool ok = (unsigned)id < (unsigned)Dm.n_pages;
+      const int len = ok ? min(max(end - key, 0), KPI) * (D * 2) : 0;
+      const int64_t off = (ok ? id : 0) * page_stride + (key & (page - 1)) * D;
+      __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc((void*)(Kp + off), 0, len, 0x00020000);
+      __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc((void*)(Vp + off), 0, len, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + i * 1024), 16, k_vo, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + i * 1024), 16, v_vo, 0, 0, 0);
+    }
+  };
+
+  // ---- fragment addresses (bytes inside a stage) -----------------------------------------------------------------------
+  const int k_row = KH == 1 ? n32 : n32 >> 1, k_half = KH == 1 ? 0 : n32 & 1;
+  const int k_base = k_row * 256 + (((k_half * 8 + hi) ^ (k_row & 15)) << 4);
+  auto k_at = [&](int base, int f) __attribute__((always_inline)) {      // fragment f: step f / 2 of a pair of 32-key blocks, block f % 2 of it
+    const int step = (f >> 1) % NKS, kb = (f >> 1) / NKS * 2 + (f & 1);
+    return (base ^ (step << 5)) + kb * (32 / KH) * 256;
+  };
+  const int vs = lane & 15, vG = lane >> 4;
+  const int v_row = KH == 1 ? (vG >> 1) * 4 + (vs >> 2) : (vG >> 1) * 2 + (vs >> 3), v_half = KH == 1 ? 0 : (vs >> 2) & 1;
+  const int v_base = PF_TILE_B + v_row * 256 + (((v_half * 8 + (vG & 1) * 2 + ((vs & 3) >> 1)) ^ ((KH == 1 ? v_row & 3 : v_row & 1) << 2)) << 4) + ((vs & 1) << 3);
+  const uint32_t ring_lds = (uint32_t)(uintptr_t)(pf_lds_u8)ring;
+
+  bf16x8 kpre[PF_KPRE];
+  auto prefetch_k = [&](int sb_off) __attribute__((always_inline)) {
+    const int base = sb_off + k_base;
+#pragma unroll
+    for (int f = 0; f < PF_KPRE; ++f) kpre[f] = *(const bf16x8*)(ring + k_at(base, f));
+  };
+  // `mid` runs before the last TAIL MFMAs are issued (all fragment reads are out by then)
+  auto s_block = [&](f32x16 (&sacc)[NKB], int sb_off, auto mid, auto tail_c) __attribute__((always_inline)) {
+    constexpr int TAIL = decltype(tail_c)::value;
+    const int base = sb_off + k_base;
+    bf16x8 kf[NKF];
+#pragma unroll
+    for (int f = 0; f < NKF; ++f) kf[f] = f < PF_KPRE ? kpre[f] : *(const bf16x8*)(ring + k_at(base, f));
+    auto mfma = [&](int f) __attribute__((always_inline)) {
+      const int step = (f >> 1) % NKS, kb = (f >> 1) / NKS * 2 + (f & 1);
+      f32x16 zero = {};
+      sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[f], qf[step], step == 0 ? zero : sacc[kb], 0, 0, 0);
+    };
+#pragma unroll
+    for (int f = 0; f < NKF - TAIL; ++f) mfma(f);
+#pragma unroll
+    for (int i = 0; i < NKF - PF_KPRE; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    if (TAIL < PF_KPRE) __builtin_amdgcn_sched_group_barrier(0x008, PF_KPRE - TAIL, 0);
+    if (TAIL > 0) {
+      mid();
+#pragma unroll
+      for (int f = NKF - TAIL; f < NKF; ++f) mfma(f);
+    }
+  };
+
+  // what the lane's row sees: key of tile t
+  auto sees = [&](int t, int key) __attribute__((always_inline)) {
+    bool s;
+    if (t < ks_.ns_t) s = key < ks_.ns && key <= pos;
+    else s = key >= ks_.w_lo && key <= pos && (Dm.window == 0 || pos - key < Dm.window || key < Dm.n_sink);
+    if (odd_pages && s) s = (unsigned)trow[key >> shift] < (unsigned)Dm.n_pages;
+    return s;
+  };
+
+  // softmax and PV of tile t, whose logits are in sacc
+  auto softmax_pv = [&](f32x16 (&sacc)[NKB], int t, int sb_off) __attribute__((always_inline)) {
+    const int kb0 = tile_key(t);
+    // does every row of the wavefront see the whole tile?
+    const bool whole = !odd_pages && (t < ks_.ns_t ? kb0 + KT <= ks_.ns : kb0 + KT - 1 <= pw0 && kb0 >= ks_.w_lo && (Dm.window == 0 || pw1 - kb0 < Dm.window));
+    bool plain = true;                         // the product on the matrix cores
+    if (!whole) {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = kb0 + kb * 32 + (r >> 2) * 8 + hi * 4 + (r & 3);
+          if (!sees(t, key)) sacc[kb][r] = -INFINITY;
+        }
+      uint32_t big = 0;                        // an exponent of ones gives bit 15 or 31
+#pragma unroll 4
+      for (int i = 0; i < PF_TILE_B / 1024; ++i) {
+        const uint4 w = *(const uint4*)(ring + sb_off + PF_TILE_B + i * 1024 + lane * 16);
+        big |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
+               ((w.w & 0x7f807f80u) + 0x00800080u);
+      }
+      plain = !__any((big & 0x80008000u) != 0);
+    }
+    uint32_t pw[NKB * 8];                      // probabilities, two keys a word
+    float ps;
+    auto exp_pack_sum = [&]() __attribute__((always_inline)) {
+      float ps0 = 0.f, ps1 = 0.f;
+      const float nm = -m_run;
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const float e0 = __builtin_amdgcn_exp2f(fmaf(sacc[kb][r], c, nm)), e1 = __builtin_amdgcn_exp2f(fmaf(sacc[kb][r + 1], c, nm));
+          pw[kb * 8 + (r >> 1)] = pack_bf16(e0, e1);
+          ps0 += e0;
+          ps1 += e1;
+        }
+      ps = ps0 + ps1;
+    };
+    auto softmax = [&]() __attribute__((always_inline)) {
+      exp_pack_sum();
+      if (__any(unset || !(ps < RESCALE_SUM))) {     // rare: set or raise the running maximum
+        float mx = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[kb][r]);
+        mx = max_across_halves(mx) * c;
+        // (a row that still sees nothing keeps maximum 0; its accumulators are 0 until it sees a key)
+        const float m_new = unset ? (mx == -INFINITY ? 0.f : mx) : fmaxf(m_run, mx);
+        const float alpha = unset ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+        unset = unset && mx == -INFINITY;
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+        exp_pack_sum();
+      }
+      l_run += ps;
+    };
+    if (plain) {
+      uint32_t va[NDB];
+      pf_s16x4 vlo[NVF], vhi[NVF];
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) va[db] = ring_lds + (uint32_t)((v_base ^ (db << 6)) + sb_off);
+#pragma unroll
+      for (int f = 0; f < VPRE; ++f) {
+        LOCRET_PF_TR(vlo[f], va[f % NDB], (f / NDB) * KC_B);
+        LOCRET_PF_TR(vhi[f], va[f % NDB], (f / NDB) * KC_B + KC_H);
+      }
+      softmax();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int f = 0; f < NVF; ++f) {
+        constexpr int LASTF = NVF - 1;
+        const int newest = f + VPRE - 1 < LASTF ? f + VPRE - 1 : LASTF;        // newest fragment already requested: two reads each behind f's
+        switch (2 * (newest - f)) {
+          case 6: LOCRET_PF_WAIT(vlo[f], vhi[f], 6); break;
+          case 4: LOCRET_PF_WAIT(vlo[f], vhi[f], 4); break;
+          case 2: LOCRET_PF_WAIT(vlo[f], vhi[f], 2); break;
+          default: LOCRET_PF_WAIT(vlo[f], vhi[f], 0); break;
+        }
+        const pf_s16x8 both = __builtin_shufflevector(vlo[f], vhi[f], 0, 1, 2, 3, 4, 5, 6, 7);
+        const int kc = f / NDB;
+        const uint4 pb = make_uint4(pw[kc * 4], pw[kc * 4 + 1], pw[kc * 4 + 2], pw[kc * 4 + 3]);
+        oacc[f % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), __builtin_bit_cast(bf16x8, pb), oacc[f % NDB], 0, 0, 0);
+        if (f + VPRE < NVF) {
+          const int fn = f + VPRE;
+          LOCRET_PF_TR(vlo[fn], va[fn % NDB], (fn / NDB) * KC_B);
+          LOCRET_PF_TR(vhi[fn], va[fn % NDB], (fn / NDB) * KC_B + KC_H);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      // a value that is not finite: key by key, for the rows that see it
+      softmax();
+#pragma unroll 1
+      for (int w = 0; w < NKB * 8; ++w) {
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < NKB * 8; ++i) mine = i == w ? pw[i] : mine;
+        const uint32_t other = __shfl_xor(mine, 32, 64);
+#pragma unroll 1
+        for (int x = 0; x < 4; ++x) {
+          const int r = (w & 7) * 2 + (x & 1), kin = (w >> 3) * 32 + (r >> 2) * 8 + (x >> 1) * 4 + (r & 3);
+          const uint32_t word = (x >> 1) == hi ? mine : other;
+          const float p = __uint_as_float((x & 1) ? word & 0xffff0000u : word << 16);
+          const bool see = sees(t, kb0 + kin);
+          const int vr = kin / KH, half = kin % KH;
+#pragma unroll
+          for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int rq = 0; rq < 4; ++rq) {
+              const int ch = half * 8 + db * 4 + rq;
+              const uint2 v = *(const uint2*)(ring + sb_off + PF_TILE_B + vr * 256 + ((ch ^ ((KH == 1 ? vr & 3 : vr & 1) << 2)) << 4) + hi * 8);
+              oacc[db][rq * 4 + 0] += see ? p * __uint_as_float(v.x << 16) : 0.f;
+              oacc[db][rq * 4 + 1] += see ? p * __uint_as_float(v.x & 0xffff0000u) : 0.f;
+              oacc[db][rq * 4 + 2] += see ? p * __uint_as_float(v.y << 16) : 0.f;
+              oacc[db][rq * 4 + 3] += see ? p * __uint_as_float(v.y & 0xffff0000u) : 0.f;
+            }
+        }
+      }
+    }
+  };
+
+  auto wg_barrier = []() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // does some row of the wavefront see some key of tile t?
+  auto active = [&](int t) __attribute__((always_inline)) {
+    const int kb = tile_key(t);
+    if (!has_rows) return false;
+    if (t < ks_.ns_t) return true;
+    return kb <= pw1 && (Dm.window == 0 || kb + KT - 1 > pw0 - Dm.window || kb < Dm.n_sink);
+  };
+  if (wave >= PF_NW / 2) {
+    load_ids(t_lo);
+    issue(t_lo, 0);
+    load_ids(t_lo + 1);
+    issue(t_lo + 1, 1);
+    load_ids(t_lo + 2);
+    issue(t_lo + 2, 2);
+    load_ids(t_lo + 3);
+    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");            // the first two tiles have landed
+    wg_barrier();
+    for (int t = t_lo; t < t_hi; ++t) {
+      const int i = t - t_lo, sb_off = (i & 3) * PF_STAGE_B;
+      wg_barrier();                                              // X
+      issue(t + 3, (i + 3) & 3);
+      load_ids(t + 4);
+      const bool act = active(t);
+      if (act) prefetch_k(sb_off);
+      wg_barrier();                                              // Y
+      if (act) {
+        f32x16 sacc[NKB];
+        s_block(sacc, sb_off, []() {}, IntC<0>());
+        softmax_pv(sacc, t, sb_off);
+      }
+      asm volatile("s_waitcnt vmcnt(8)" ::: "memory");          // own loads of tile t + 2 have landed
+    }
+  } else {
+    wg_barrier();
+    prefetch_k(0);
+    for (int t = t_lo; t < t_hi; ++t) {
+      const int i = t - t_lo, sb_off = (i & 3) * PF_STAGE_B;
+      wg_barrier();                                              // X
+      if (active(t)) {
+        f32x16 sacc[NKB];
+        s_block(sacc, sb_off, wg_barrier, IntC<YTAIL>());        // Y inside
+        softmax_pv(sacc, t, sb_off);
+      } else {
+        wg_barrier();                                            // Y
+      }
+      prefetch_k(((i + 1) & 3) * PF_STAGE_B);
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // trailing empty loads
+
+  // ---- results ---------------------------------------------------------------------------------------------------------
+  const float l = l_run + __shfl_xor(l_run, 32, 64);
+  if (cut) {
+    const int64_t slot = blockIdx.x;
+    float4* op = (float4*)part + (slot * PF_NW + wave) * (NDB * 4 * 64) + lane;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq)
+        op[(db * 4 + rq) * 64] = make_float4(oacc[db][rq * 4 + 0], oacc[db][rq * 4 + 1], oacc[db][rq * 4 + 2], oacc[db][rq * 4 + 3]);
+    if (hi == 0) ((float2*)(part + (int64_t)PF_MAX_SLOTS * PF_ROWS * D))[slot * PF_ROWS + wave * 32 + n32] = make_float2(m_run, l);
+  } else if (wave * 32 + n32 < rows) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;      // a row that sees nothing
+    bf16_t* op = (bf16_t*)a.out + at * D;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int rq = 0; rq < 4; ++rq) {
+        uint2 w;
+        w.x = pack_bf16(oacc[db][rq * 4 + 0] * inv, oacc[db][rq * 4 + 1] * inv);
+        w.y = pack_bf16(oacc[db][rq * 4 + 2] * inv, oacc[db][rq * 4 + 3] * inv);
+        *(uint2*)(op + db * 32 + rq * 8 + hi * 4) = w;
+      }
+    if (a.lse && hi == 0) a.lse[at] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  }
+}
+
+// out = sum_p w_p O_p / sum_p w_p l_p, w_p = 2^(m_p - max m), over the parts of an item that was cut.  One workgroup per (item, 32 dims), its
+// threads as in the attention kernel.
+template <int D>
+__global__ __launch_bounds__(PF_THREADS) void paged_prefill_join_kernel(PagedAttn a, PagedDims Dm, int n_items, int parts, const float* __restrict__ part) {
+  constexpr int NDB = D / 32;
+  extern __shared__ int32_t first[];
+  PfItem it;
+  if (!pf_item(a, Dm, blockIdx.x, first, it)) return;
+  const PfKeys k = pf_keys(it, Dm, pf_tile_keys(D));
+  const int len = pf_part_len(k.n_tiles, parts), n = (k.n_tiles + len - 1) / len;
+  if (n <= 1) return;
+  const int db = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n32 = lane & 31, hi = lane >> 5;
+  const int row = wave * 32 + n32;
+  const float2* ml = (const float2*)(part + (int64_t)PF_MAX_SLOTS * PF_ROWS * D) + row;
+  const float4* op = (const float4*)part + (int64_t)wave * (NDB * 4 * 64) + db * (4 * 64) + lane;
+  float M = -INFINITY;
+  for (int p = 0; p < n; ++p) {
+    const float2 x = ml[((int64_t)p * n_items + blockIdx.x) * PF_ROWS];
+    if (x.y != 0.f) M = fmaxf(M, x.x);
+  }
+  float acc[16], den = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+  for (int p = 0; p < n; ++p) {
+    const int64_t slot = (int64_t)p * n_items + blockIdx.x;
+    const float2 x = ml[slot * PF_ROWS];
+    if (x.y == 0.f) continue;                        // saw nothing (a sum of NaN is not 0)
+    const float w = __builtin_amdgcn_exp2f(x.x - M);
+    den = fmaf(w, x.y, den);
+#pragma unroll
+    for (int rq = 0; rq < 4; ++rq) {
+      const float4 o = op[slot * (PF_NW * NDB * 4 * 64) + rq * 64];
+      acc[rq * 4 + 0] = fmaf(w, o.x, acc[rq * 4 + 0]);
+      acc[rq * 4 + 1] = fmaf(w, o.y, acc[rq * 4 + 1]);
+      acc[rq * 4 + 2] = fmaf(w, o.z, acc[rq * 4 + 2]);
+      acc[rq * 4 + 3] = fmaf(w, o.w, acc[rq * 4 + 3]);
+    }
+  }
+  if (row >= it.n_tok * Dm.g) return;
+  const int64_t at = (int64_t)(it.t0 + row / Dm.g) * Dm.h + it.m * Dm.g + row % Dm.g;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  bf16_t* dst = (bf16_t*)a.out + at * D + db * 32 + hi * 4;
+#pragma unroll
+  for (int rq = 0; rq < 4; ++rq) {
+    uint2 w;
+    w.x = pack_bf16(acc[rq * 4 + 0] * inv, acc[rq * 4 + 1] * inv);
+    w.y = pack_bf16(acc[rq * 4 + 2] * inv, acc[rq * 4 + 3] * inv);
+    *(uint2*)(dst + rq * 8) = w;
+  }
+  if (a.lse && hi == 0 && db == 0) a.lse[at] = den == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(den)) * 0.6931471805599453f;
+}
+
+size_t paged_prefill_workspace(const PagedDims& D) { return D.bf16 ? (size_t)PF_MAX_SLOTS * PF_ROWS * (D.d + 2) * sizeof(float) : 0; }
+
+template <int D>
+static void prefill_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t st) {
+  const int tw = PF_ROWS / Dm.g;
+  // token tiles at most: every request's last one may be short
+  int64_t tiles = ((int64_t)a.T + (int64_t)a.n_req * (tw - 1)) / tw;
+  if (tiles > a.T) tiles = a.T;
+  const int n_items = (int)(tiles * Dm.h_kv);
+  int parts = PF_CUS / n_items;
+  parts = parts < 1 ? 1 : parts > PF_MAX_PARTS ? PF_MAX_PARTS : parts;
+  paged_prefill_kernel<D><<<(unsigned)n_items * (unsigned)parts, PF_THREADS, 0, st>>>(a, a.table, Dm, n_items, parts, (float*)a.ws);
+  if (parts > 1)
+    paged_prefill_join_kernel<D><<<dim3((unsigned)n_items, D / 32), PF_THREADS, (size_t)(a.n_req + 1) * sizeof(int32_t), st>>>(a, Dm, n_items, parts, (const float*)a.ws);
+}
+
+void launch_paged_prefill(const PagedDims& D, const PagedAttn& a, hipStream_t st) {
+  switch (D.d) {
+    case 32: prefill_d<32>(D, a, st); break;
+    case 64: prefill_d<64>(D, a, st); break;
+    case 96: prefill_d<96>(D, a, st); break;
+    default: prefill_d<128>(D, a, st); break;
+  }
+}
+
+}  // namespace locret
