@@ -25,8 +25,8 @@
 // a key, and raised when the row's sum over a tile reaches 2^30.  Probabilities become bf16 factors, half a step of 2^-8 each; sums, maxima
 // and accumulators are 32-bit.
 // Tiles that some row of a wavefront does not see whole are masked before the maximum.  A masked probability is 0, but 0 times a value that is
-// not finite is not, so such a tile's values are looked through first, and if one is not finite the tile's product is
-// formed key by key for the rows that see it.
+// not finite is not, so such a tile's values are looked through, and if one is not finite the wavefront forms its rows once more after the loop,
+// key by key (there, where no tile's registers are alive; the same for the one tile, inside the loop, took half of its speed in spills).
 //
 // Few rows: where the items (tokens tile, KV head) are at most half as many as the CUs, each one's keys are cut into parts,
 // workgroups of their own, which leave maximum, sum and accumulators; a second launch joins them.
@@ -185,6 +185,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const float c = Dm.scale * 1.4426950408889634f;
   float m_run = 0.f, l_run = 0.f;              // of the lane's row, in log2 units; the sum over this lane's keys
   bool unset = true;                           // the row has seen no key yet
+  bool redo = false;                           // the wavefront's rows have to be formed key by key
 
   // ---- tiles -----------------------------------------------------------------------------------------------------------
   auto tile_key = [&](int t) __attribute__((always_inline)) { return t < ks_.ns_t ? t * KT : ks_.wb + (t - ks_.ns_t) * KT; };
@@ -284,7 +285,6 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     const int kb0 = tile_key(t);
     // does every row of the wavefront see the whole tile?
     const bool whole = !odd_pages && (t < ks_.ns_t ? kb0 + KT <= ks_.ns : kb0 + KT - 1 <= pw0 && kb0 >= ks_.w_lo && (Dm.window == 0 || pw1 - kb0 < Dm.window));
-    bool plain = true;                         // the product on the matrix cores
     if (!whole) {
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
         big |= ((w.x & 0x7f807f80u) + 0x00800080u) | ((w.y & 0x7f807f80u) + 0x00800080u) | ((w.z & 0x7f807f80u) + 0x00800080u) |
                ((w.w & 0x7f807f80u) + 0x00800080u);
       }
-      plain = !__any((big & 0x80008000u) != 0);
+      redo = redo || __any((big & 0x80008000u) != 0);
     }
     uint32_t pw[NKB * 8];                      // probabilities, two keys a word
     float ps;
@@ -341,68 +341,37 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
       }
       l_run += ps;
     };
-    if (plain) {
-      uint32_t va[NDB];
-      pf_s16x4 vlo[NVF], vhi[NVF];
+    uint32_t va[NDB];
+    pf_s16x4 vlo[NVF], vhi[NVF];
 #pragma unroll
-      for (int db = 0; db < NDB; ++db) va[db] = ring_lds + (uint32_t)((v_base ^ (db << 6)) + sb_off);
+    for (int db = 0; db < NDB; ++db) va[db] = ring_lds + (uint32_t)((v_base ^ (db << 6)) + sb_off);
 #pragma unroll
-      for (int f = 0; f < VPRE; ++f) {
-        LOCRET_PF_TR(vlo[f], va[f % NDB], (f / NDB) * KC_B);
-        LOCRET_PF_TR(vhi[f], va[f % NDB], (f / NDB) * KC_B + KC_H);
+    for (int f = 0; f < VPRE; ++f) {
+      LOCRET_PF_TR(vlo[f], va[f % NDB], (f / NDB) * KC_B);
+      LOCRET_PF_TR(vhi[f], va[f % NDB], (f / NDB) * KC_B + KC_H);
+    }
+    softmax();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int f = 0; f < NVF; ++f) {
+      constexpr int LASTF = NVF - 1;
+      const int newest = f + VPRE - 1 < LASTF ? f + VPRE - 1 : LASTF;        // newest fragment already requested: two reads each behind f's
+      switch (2 * (newest - f)) {
+        case 6: LOCRET_PF_WAIT(vlo[f], vhi[f], 6); break;
+        case 4: LOCRET_PF_WAIT(vlo[f], vhi[f], 4); break;
+        case 2: LOCRET_PF_WAIT(vlo[f], vhi[f], 2); break;
+        default: LOCRET_PF_WAIT(vlo[f], vhi[f], 0); break;
       }
-      softmax();
+      const pf_s16x8 both = __builtin_shufflevector(vlo[f], vhi[f], 0, 1, 2, 3, 4, 5, 6, 7);
+      const int kc = f / NDB;
+      const uint4 pb = make_uint4(pw[kc * 4], pw[kc * 4 + 1], pw[kc * 4 + 2], pw[kc * 4 + 3]);
+      oacc[f % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), __builtin_bit_cast(bf16x8, pb), oacc[f % NDB], 0, 0, 0);
+      if (f + VPRE < NVF) {
+        const int fn = f + VPRE;
+        LOCRET_PF_TR(vlo[fn], va[fn % NDB], (fn / NDB) * KC_B);
+        LOCRET_PF_TR(vhi[fn], va[fn % NDB], (fn / NDB) * KC_B + KC_H);
+      }
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int f = 0; f < NVF; ++f) {
-        constexpr int LASTF = NVF - 1;
-        const int newest = f + VPRE - 1 < LASTF ? f + VPRE - 1 : LASTF;        // newest fragment already requested: two reads each behind f's
-        switch (2 * (newest - f)) {
-          case 6: LOCRET_PF_WAIT(vlo[f], vhi[f], 6); break;
-          case 4: LOCRET_PF_WAIT(vlo[f], vhi[f], 4); break;
-          case 2: LOCRET_PF_WAIT(vlo[f], vhi[f], 2); break;
-          default: LOCRET_PF_WAIT(vlo[f], vhi[f], 0); break;
-        }
-        const pf_s16x8 both = __builtin_shufflevector(vlo[f], vhi[f], 0, 1, 2, 3, 4, 5, 6, 7);
-        const int kc = f / NDB;
-        const uint4 pb = make_uint4(pw[kc * 4], pw[kc * 4 + 1], pw[kc * 4 + 2], pw[kc * 4 + 3]);
-        oacc[f % NDB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), __builtin_bit_cast(bf16x8, pb), oacc[f % NDB], 0, 0, 0);
-        if (f + VPRE < NVF) {
-          const int fn = f + VPRE;
-          LOCRET_PF_TR(vlo[fn], va[fn % NDB], (fn / NDB) * KC_B);
-          LOCRET_PF_TR(vhi[fn], va[fn % NDB], (fn / NDB) * KC_B + KC_H);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-      // a value that is not finite: key by key, for the rows that see it
-      softmax();
-#pragma unroll 1
-      for (int w = 0; w < NKB * 8; ++w) {
-        uint32_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < NKB * 8; ++i) mine = i == w ? pw[i] : mine;
-        const uint32_t other = __shfl_xor(mine, 32, 64);
-#pragma unroll 1
-        for (int x = 0; x < 4; ++x) {
-          const int r = (w & 7) * 2 + (x & 1), kin = (w >> 3) * 32 + (r >> 2) * 8 + (x >> 1) * 4 + (r & 3);
-          const uint32_t word = (x >> 1) == hi ? mine : other;
-          const float p = __uint_as_float((x & 1) ? word & 0xffff0000u : word << 16);
-          const bool see = sees(t, kb0 + kin);
-          const int vr = kin / KH, half = kin % KH;
-#pragma unroll
-          for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int rq = 0; rq < 4; ++rq) {
-              const int ch = half * 8 + db * 4 + rq;
-              const uint2 v = *(const uint2*)(ring + sb_off + PF_TILE_B + vr * 256 + ((ch ^ ((KH == 1 ? vr & 3 : vr & 1) << 2)) << 4) + hi * 8);
-              oacc[db][rq * 4 + 0] += see ? p * __uint_as_float(v.x << 16) : 0.f;
-              oacc[db][rq * 4 + 1] += see ? p * __uint_as_float(v.x & 0xffff0000u) : 0.f;
-              oacc[db][rq * 4 + 2] += see ? p * __uint_as_float(v.y << 16) : 0.f;
-              oacc[db][rq * 4 + 3] += see ? p * __uint_as_float(v.y & 0xffff0000u) : 0.f;
-            }
-        }
-      }
     }
   };
 
@@ -460,6 +429,51 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     }
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // trailing empty loads
+
+  if (redo) {
+    // A masked value that is not finite has met the matrix cores.  The wavefront's rows again, key by key: a lane has the dims of its
+    // row that its accumulators hold.
+    float qv[NDB][16];
+    const bf16_t* qp = (const bf16_t*)a.q + at * D + hi * 4;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        qv[db][r] = bf2f(qp[db * 32 + (r >> 2) * 8 + (r & 3)]);
+        oacc[db][r] = 0.f;
+      }
+    m_run = -INFINITY;
+    float l = 0.f;
+#pragma unroll 1
+    for (int t = t_lo; t < t_hi; ++t) {
+      if (!active(t)) continue;
+      const int kb0 = tile_key(t), end = min(t < ks_.ns_t ? ks_.ns : ks_.n_keys, kb0 + KT);
+#pragma unroll 1
+      for (int key = kb0; key < end; ++key) {
+        const int id = __builtin_amdgcn_readfirstlane(trow[key >> shift]);
+        if ((unsigned)id >= (unsigned)Dm.n_pages) continue;
+        const int64_t off = id * page_stride + (key & (page - 1)) * D + hi * 4;
+        float s = 0.f;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s = fmaf(qv[db][r], bf2f(Kp[off + db * 32 + (r >> 2) * 8 + (r & 3)]), s);
+        s += __shfl_xor(s, 32, 64);
+        const bool see = sees(t, key);
+        const float x = see ? s * c : -INFINITY, m_new = fmaxf(m_run, x), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - ref), p = __builtin_amdgcn_exp2f(x - ref);
+        l = l * alpha + p;
+        m_run = m_new;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            oacc[db][r] = oacc[db][r] * alpha + (see ? p * bf2f(Vp[off + db * 32 + (r >> 2) * 8 + (r & 3)]) : 0.f);
+      }
+    }
+    if (m_run == -INFINITY) m_run = 0.f;
+    l_run = hi ? 0.f : l;
+  }
 
   // ---- results ---------------------------------------------------------------------------------------------------------
   const float l = l_run + __shfl_xor(l_run, 32, 64);
