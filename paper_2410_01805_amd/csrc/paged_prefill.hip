@@ -37,6 +37,8 @@ namespace locret {
 
 typedef __attribute__((address_space(3))) void* pf_lds_ptr;
 typedef __attribute__((address_space(3))) unsigned char* pf_lds_u8;
+// The block table, read through the scalar cache where the index is the same in the wavefront.
+typedef const __attribute__((address_space(4))) int32_t* pf_table;
 typedef short pf_s16x4 __attribute__((ext_vector_type(4)));
 typedef short pf_s16x8 __attribute__((ext_vector_type(8)));
 
@@ -153,6 +155,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const int g = Dm.g, shift = Dm.page_shift, page = 1 << shift;
   const int rows = it.n_tok * g;
   const int32_t* trow = table + (int64_t)it.r * Dm.max_pages;
+  const pf_table trow_s = (pf_table)(uint64_t)trow;
 
   // pages that are not the pool's, among those of the item's keys
   bool odd_pages;
@@ -197,6 +200,11 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const int64_t page_stride = (int64_t)Dm.h_kv * page * D;
   const bf16_t* Kp = (const bf16_t*)a.K + (int64_t)it.m * page * D;
   const bf16_t* Vp = (const bf16_t*)a.V + (int64_t)it.m * page * D;
+  auto scalar_ptr = [](const bf16_t* p) -> void* {
+    const uint64_t x = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), up = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));    // (the builtin is signed)
+    return (void*)(((uint64_t)up << 32) | lo);
+  };
   int ids[4];                                                    // page numbers of the tile that is loaded next
   auto load_ids = [&](int t) __attribute__((always_inline)) {
     const int tu = __builtin_amdgcn_readfirstlane(t);
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     for (int u = 0; u < 4; ++u) {
       const int key = kb + (w4 + u * 4) * KPI;
       ids[u] = -1;
-      if (key < end) ids[u] = trow[key >> shift];
+      if (key < end) ids[u] = trow_s[key >> shift];
     }
   };
   auto issue = [&](int t, int stage) __attribute__((always_inline)) {
@@ -217,10 +225,10 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
       const int i = w4 + u * 4, key = kb + i * KPI;
       const int id = __builtin_amdgcn_readfirstlane(ids[u]);
       const bool ok = (unsigned)id < (unsigned)Dm.n_pages;
-      const int len = ok ? min(max(end - key, 0), KPI) * (D * 2) : 0;
+      const int len = __builtin_amdgcn_readfirstlane(ok ? min(max(end - key, 0), KPI) * (D * 2) : 0);
       const int64_t off = (ok ? id : 0) * page_stride + (key & (page - 1)) * D;
-      __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc((void*)(Kp + off), 0, len, 0x00020000);
-      __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc((void*)(Vp + off), 0, len, 0x00020000);
+      __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Kp + off), 0, len, 0x00020000);
+      __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Vp + off), 0, len, 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + i * 1024), 16, k_vo, 0, 0, 0);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + i * 1024), 16, v_vo, 0, 0, 0);
     }
