@@ -110,12 +110,13 @@ __device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm,
 struct PfKeys {
   int n_keys, w_lo, ns, wb, ns_t, n_tiles;
 };
+// (Tiles start at multiples of 16, or of their own length where a page holds one.)
 __device__ __forceinline__ PfKeys pf_keys(const PfItem& it, const PagedDims& Dm, int KT) {
   PfKeys k;
   k.n_keys = max(it.p0 + it.n_tok, 0);                    // (positions below 0 see nothing)
   k.w_lo = Dm.window ? max(0, it.p0 - Dm.window + 1) : 0;
   k.ns = min(Dm.n_sink, k.w_lo);
-  k.wb = k.w_lo & ~15;
+  k.wb = k.w_lo & ~((1 << Dm.page_shift >= KT ? KT : 16) - 1);
   k.ns_t = (k.ns + KT - 1) / KT;
   k.n_tiles = k.ns_t + (max(k.n_keys - k.wb, 0) + KT - 1) / KT;
   return k;
@@ -197,18 +198,27 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   constexpr int OUTSIDE = 0x7ffff000;                            // an offset no descriptor reaches: the load brings zeros
   auto offset = [&](int ch) { return ch % SLOT < NCH ? (l_row * KH + ch / SLOT) * (D * 2) + ch % SLOT * 16 : OUTSIDE; };
   const int k_vo = offset(l_pos ^ l_row ^ (w4 << 2)), v_vo = offset(l_pos ^ ((KH == 1 ? l_row : l_row & 1) << 2));
-  const int64_t page_stride = (int64_t)Dm.h_kv * page * D;
-  const bf16_t* Kp = (const bf16_t*)a.K + (int64_t)it.m * page * D;
-  const bf16_t* Vp = (const bf16_t*)a.V + (int64_t)it.m * page * D;
-  auto scalar_ptr = [](const bf16_t* p) -> void* {
+  const uint32_t page_b = (uint32_t)(Dm.h_kv * page) * (D * 2);          // (at most 1024 heads x 256 units x 256 bytes)
+  const unsigned char* Kp = (const unsigned char*)a.K + (int64_t)it.m * page * (D * 2);
+  const unsigned char* Vp = (const unsigned char*)a.V + (int64_t)it.m * page * (D * 2);
+  auto scalar_ptr = [](const unsigned char* p) -> void* {
     const uint64_t x = (uint64_t)p;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), up = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));    // (the builtin is signed)
     return (void*)(((uint64_t)up << 32) | lo);
   };
-  int ids[4];                                                    // page numbers of the tile that is loaded next
+  // Page numbers of the tile that is loaded next.  Where a page holds whole tiles there is one, and one descriptor for all loads; else one for
+  // each load instruction.  (The second form takes some 150 scalar instructions a tile, which outlast A's S block: a 4096-token chunk on 16384
+  // units, pages of 64, 1000 us instead of 800.)
+  const bool one_page = page >= KT;
+  int ids[4];
   auto load_ids = [&](int t) __attribute__((always_inline)) {
     const int tu = __builtin_amdgcn_readfirstlane(t);
     const int kb = tile_key(tu), end = tu >= t_hi ? 0 : tu < ks_.ns_t ? ks_.ns : ks_.n_keys;
+    if (one_page) {
+      ids[0] = -1;
+      if (kb < end) ids[0] = trow_s[kb >> shift];
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int key = kb + (w4 + u * 4) * KPI;
@@ -219,18 +229,34 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   auto issue = [&](int t, int stage) __attribute__((always_inline)) {
     const int tu = __builtin_amdgcn_readfirstlane(t);
     const int kb = tile_key(tu), end = tu >= t_hi ? 0 : tu < ks_.ns_t ? ks_.ns : ks_.n_keys;
-    unsigned char* sb = ring + stage * PF_STAGE_B;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int i = w4 + u * 4, key = kb + i * KPI;
-      const int id = __builtin_amdgcn_readfirstlane(ids[u]);
-      const bool ok = (unsigned)id < (unsigned)Dm.n_pages;
-      const int len = __builtin_amdgcn_readfirstlane(ok ? min(max(end - key, 0), KPI) * (D * 2) : 0);
-      const int64_t off = (ok ? id : 0) * page_stride + (key & (page - 1)) * D;
+    unsigned char* sb = ring + stage * PF_STAGE_B + w4 * 1024;
+    if (one_page) {
+      const uint32_t id = __builtin_amdgcn_readfirstlane(ids[0]);
+      const bool ok = id < (uint32_t)Dm.n_pages;
+      const int len = __builtin_amdgcn_readfirstlane(ok ? min(max(end - kb, 0), KT) * (D * 2) : 0);
+      const uint64_t off = (uint64_t)(ok ? id : 0u) * page_b + (uint32_t)((kb & (page - 1)) * (D * 2));
       __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Kp + off), 0, len, 0x00020000);
       __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Vp + off), 0, len, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + i * 1024), 16, k_vo, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + i * 1024), 16, v_vo, 0, 0, 0);
+      const int first = w4 * (KPI * D * 2);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + u * 4096), 16, k_vo, first + u * (4 * KPI * D * 2), 0, 0);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + u * 4096), 16, v_vo, first + u * (4 * KPI * D * 2), 0, 0);
+      return;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int key = kb + (w4 + u * 4) * KPI;
+      const uint32_t id = __builtin_amdgcn_readfirstlane(ids[u]);
+      const bool ok = id < (uint32_t)Dm.n_pages;
+      const int len = __builtin_amdgcn_readfirstlane(ok ? min(max(end - key, 0), KPI) * (D * 2) : 0);
+      const uint64_t off = (uint64_t)(ok ? id : 0u) * page_b + (uint32_t)((key & (page - 1)) * (D * 2));
+      __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Kp + off), 0, len, 0x00020000);
+      __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Vp + off), 0, len, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + u * 4096), 16, k_vo, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + u * 4096), 16, v_vo, 0, 0, 0);
     }
   };
 
@@ -460,12 +486,13 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
       for (int key = kb0; key < end; ++key) {
         const int id = __builtin_amdgcn_readfirstlane(trow[key >> shift]);
         if ((unsigned)id >= (unsigned)Dm.n_pages) continue;
-        const int64_t off = id * page_stride + (key & (page - 1)) * D + hi * 4;
+        const int64_t off = (int64_t)id * page_b + (key & (page - 1)) * (D * 2) + hi * 8;
+        const bf16_t *kr = (const bf16_t*)(Kp + off), *vr = (const bf16_t*)(Vp + off);
         float s = 0.f;
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s = fmaf(qv[db][r], bf2f(Kp[off + db * 32 + (r >> 2) * 8 + (r & 3)]), s);
+          for (int r = 0; r < 16; ++r) s = fmaf(qv[db][r], bf2f(kr[db * 32 + (r >> 2) * 8 + (r & 3)]), s);
         s += __shfl_xor(s, 32, 64);
         const bool see = sees(t, key);
         const float x = see ? s * c : -INFINITY, m_new = fmaxf(m_run, x), ref = m_new == -INFINITY ? 0.f : m_new;
@@ -476,7 +503,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            oacc[db][r] = oacc[db][r] * alpha + (see ? p * bf2f(Vp[off + db * 32 + (r >> 2) * 8 + (r & 3)]) : 0.f);
+            oacc[db][r] = oacc[db][r] * alpha + (see ? p * bf2f(vr[db * 32 + (r >> 2) * 8 + (r & 3)]) : 0.f);
       }
     }
     if (m_run == -INFINITY) m_run = 0.f;

@@ -343,11 +343,12 @@ def test_prefill_follows_its_definition(dtype, h, h_kv, d, page, lens, new, wind
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 96), ("bf16", 64), ("bf16", 32), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("window,sink", [(0, 0), (40, 5)])
 @pytest.mark.parametrize("what", ["nan", "inf", "lowest"])
-def test_what_is_masked_does_not_reach_the_result(dtype, d, window, sink, what):
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_what_is_masked_does_not_reach_the_result(dtype, d, window, sink, what, page):
     """Not-a-number, infinite and lowest values behind the lengths, in later tokens and in front of the window; the tokens that do see such a
     value row get what the definition gives them."""
     rng = np.random.default_rng(d + window)
-    lens, new, page = [150, 37, 64], [100, 37, 3], 16
+    lens, new = [150, 37, 64], [100, 37, 3]
     c = paged_case(rng, dtype, 4, 2, d, page, lens, window, sink)
     bad = {"nan": float("nan"), "inf": float("inf"), "lowest": torch.finfo(tt(dtype)).min}[what]
     at = [(0, 120), (0, 60), (1, 20), (2, 63), (2, 9), (0, 149)]
@@ -360,6 +361,7 @@ def test_what_is_masked_does_not_reach_the_result(dtype, d, window, sink, what):
     for r, n in enumerate(lens):                           # behind the lengths, keys too
         p, i = c["table"][r, (n - 1) // page], (n - 1) % page + 1
         c["V"][p, :, i:], c["K"][p, :, i:] = bad, bad
+        c["V64"][p, :, i:], c["K64"][p, :, i:] = bad, bad
     spare = [p for p in range(c["K"].shape[0]) if p not in {c["table"][r, k] for r, n in enumerate(lens) for k in range(-(-n // page))}]
     for p in spare:
         c["K"][p], c["V"][p] = bad, bad
@@ -377,11 +379,12 @@ def test_what_is_masked_does_not_reach_the_result(dtype, d, window, sink, what):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_pages_outside_the_pool_are_not_seen(dtype):
+@pytest.mark.parametrize("page", [16, 64, 128])
+def test_pages_outside_the_pool_are_not_seen(dtype, page):
     rng = np.random.default_rng(11)
-    c = paged_case(rng, dtype, 4, 2, 64, 16, [150, 40, 20])
+    c = paged_case(rng, dtype, 4, 2, 64, page, [150 * page // 16, 40, 20])
     c["table"][0, [2, 5]] = [-1, 1 << 27]
-    c["table"][1, :3] = c["K"].shape[0]                    # nothing is left of this request
+    c["table"][1, : -(-40 // page)] = c["K"].shape[0]      # nothing is left of this request
     new = [9, 40, 2]
     q, q64 = numbers(rng, dtype, sum(new), 4, 64)
     out, lse = run_prefill(c, q, np.cumsum([0] + new))
