@@ -37,8 +37,6 @@ namespace locret {
 
 typedef __attribute__((address_space(3))) void* pf_lds_ptr;
 typedef __attribute__((address_space(3))) unsigned char* pf_lds_u8;
-// The block table, read through the scalar cache where the index is the same in the wavefront.
-typedef const __attribute__((address_space(4))) int32_t* pf_table;
 typedef short pf_s16x4 __attribute__((ext_vector_type(4)));
 typedef short pf_s16x8 __attribute__((ext_vector_type(8)));
 
@@ -58,9 +56,12 @@ struct PfItem {
 #define LOCRET_PF_WAIT(a, b, n) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "i"(n))
 
 // Finds item x = (token tile, KV head): the token tiles of all requests in their order, a request's last tile first (it sees the most keys).
-// first: LDS, n_req + 1 ints, free again after the next barrier.  False: there is no such tile.  All results are the same in the whole workgroup.
-__device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm, int x, int32_t* first, PfItem& it) {
-  __shared__ int64_t scan[PF_NW];
+// scratch: LDS, PF_NW 64-bit words and n_req + 1 ints, free again after the next barrier.  False: there is no such tile.  All results are the
+// same in the whole workgroup.
+constexpr int PF_SCRATCH = PF_NW * 8;
+__device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm, int x, unsigned char* scratch, PfItem& it) {
+  int64_t* scan = (int64_t*)scratch;
+  int32_t* first = (int32_t*)(scratch + PF_SCRATCH);
   const int tid = threadIdx.x, tw = PF_ROWS / Dm.g, ipt = (a.n_req + PF_THREADS - 1) / PF_THREADS;
   int64_t mine = 0, total;
   for (int u = 0; u < ipt; ++u) {
@@ -126,9 +127,10 @@ __device__ __forceinline__ int pf_part_len(int n_tiles, int k) { return max((n_t
 
 __host__ __device__ constexpr int pf_tile_keys(int d) { return d <= 64 ? 128 : 64; }
 
-template <int D>
-__global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm, int n_items,
-                                                                     int parts, float* __restrict__ part) {
+template <int D, bool ONE_PAGE>
+__global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn a, const bf16_t* __restrict__ q, const bf16_t* __restrict__ K,
+                                                                     const bf16_t* __restrict__ V, const int32_t* __restrict__ table, PagedDims Dm,
+                                                                     int n_items, int parts, float* __restrict__ part) {
   constexpr int KH = D <= 64 ? 2 : 1;                      // keys of an LDS row
   constexpr int KT = 64 * KH, NKB = KT / 32;               // keys and 32-key blocks of a tile
   constexpr int NKS = D / 16, NDB = D / 32;                // contraction steps of S, 32-dim blocks of O^T
@@ -136,11 +138,13 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   constexpr int VPRE = KH == 2 ? 2 : 4;                    // V^T fragments in flight ahead of their MFMA
   constexpr int KC_B = 4096 / KH, KC_H = 2048 / KH;        // bytes of 16 keys and of 8 keys in LDS
   constexpr int YTAIL = D == 128 ? 4 : 1;                  // MFMAs of A's S block behind barrier Y
+  // The only LDS variable: with a second one the compiler tells them apart by alias scopes, and then waits for all direct loads before every
+  // read of `ring`, which it cannot tell from the stages in flight (4096 tokens on 16384 units: 909 us instead of @@).
   __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * PF_STAGE_B];
 
   PfItem it;
   const int layer = blockIdx.x / n_items;
-  if (!pf_item(a, Dm, blockIdx.x - layer * n_items, (int32_t*)ring, it)) return;
+  if (!pf_item(a, Dm, blockIdx.x - layer * n_items, ring, it)) return;
   const PfKeys ks_ = pf_keys(it, Dm, KT);
   int t_lo = 0, t_hi = ks_.n_tiles;
   bool cut = false;
@@ -156,8 +160,9 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const int g = Dm.g, shift = Dm.page_shift, page = 1 << shift;
   const int rows = it.n_tok * g;
   const int32_t* trow = table + (int64_t)it.r * Dm.max_pages;
-  const pf_table trow_s = (pf_table)(uint64_t)trow;
 
+  auto tile_key = [&](int t) __attribute__((always_inline)) { return t < ks_.ns_t ? t * KT : ks_.wb + (t - ks_.ns_t) * KT; };
+  auto tile_end = [&](int t) __attribute__((always_inline)) { return t >= t_hi ? 0 : t < ks_.ns_t ? ks_.ns : ks_.n_keys; };
   // pages that are not the pool's, among those of the item's keys
   bool odd_pages;
   {
@@ -165,7 +170,14 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     const int s_end = (ks_.ns + page - 1) >> shift, e0 = ks_.wb >> shift, e1 = (ks_.n_keys + page - 1) >> shift;
     for (int i = tid; i < s_end; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
     for (int i = e0 + tid; i < e1; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
-    odd_pages = __syncthreads_or(odd);                     // (also: `ring` no longer holds the sums of pf_item)
+    int32_t* said = (int32_t*)ring;
+    __syncthreads();                                       // `ring` no longer holds the sums of pf_item
+    if (tid == 0) *said = 0;
+    __syncthreads();
+    if (odd) *said = 1;
+    __syncthreads();
+    odd_pages = __builtin_amdgcn_readfirstlane(*said) != 0;
+    __syncthreads();
   }
 
   // this lane's row, and the first and last position of the wavefront's
@@ -173,13 +185,18 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const int64_t at = (int64_t)(it.t0 + tok) * Dm.h + it.m * g + (row - tok * g);
   const int pos = it.p0 + tok;
   const int pw0 = it.p0 + min(wave * 32, rows - 1) / g, pw1 = it.p0 + min(wave * 32 + 31, rows - 1) / g;
-  const bool has_rows = wave * 32 < rows;
+  // first keys of the tiles that all rows of the wavefront see whole (among the sinks: up to all_sink), and of those that some row sees a key of
+  const int all_lo = Dm.window ? max(ks_.w_lo, pw1 - Dm.window + 1) : 0, all_hi = odd_pages ? -1 : pw0 - KT + 1, all_sink = odd_pages ? -1 : ks_.ns - KT;
+  const int any_lo = Dm.window ? pw0 - Dm.window - KT + 2 : 0, any_hi = wave * 32 < rows ? pw1 : -1;
 
   bf16x8 qf[NKS];
   {
-    const bf16_t* qp = (const bf16_t*)a.q + at * D + hi * 8;
+    const bf16_t* qp = q + at * D + hi * 8;
 #pragma unroll
     for (int s = 0; s < NKS; ++s) qf[s] = *(const bf16x8*)(qp + s * 16);
+    // waited for here: a wait in the loop, where they are used first, would be one for the tiles in flight too
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) asm volatile("" : "+v"(qf[s]));
   }
   f32x16 oacc[NDB];
 #pragma unroll
@@ -192,71 +209,68 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   bool redo = false;                           // the wavefront's rows have to be formed key by key
 
   // ---- tiles -----------------------------------------------------------------------------------------------------------
-  auto tile_key = [&](int t) __attribute__((always_inline)) { return t < ks_.ns_t ? t * KT : ks_.wb + (t - ks_.ns_t) * KT; };
   const int w4 = wave & 3, l_row = lane >> 4, l_pos = lane & 15;
   constexpr int NCH = D / 8, SLOT = 16 / KH, KPI = 4 * KH;       // chunks of a key in memory and in LDS; keys of a load instruction
   constexpr int OUTSIDE = 0x7ffff000;                            // an offset no descriptor reaches: the load brings zeros
   auto offset = [&](int ch) { return ch % SLOT < NCH ? (l_row * KH + ch / SLOT) * (D * 2) + ch % SLOT * 16 : OUTSIDE; };
   const int k_vo = offset(l_pos ^ l_row ^ (w4 << 2)), v_vo = offset(l_pos ^ ((KH == 1 ? l_row : l_row & 1) << 2));
   const uint32_t page_b = (uint32_t)(Dm.h_kv * page) * (D * 2);          // (at most 1024 heads x 256 units x 256 bytes)
-  const unsigned char* Kp = (const unsigned char*)a.K + (int64_t)it.m * page * (D * 2);
-  const unsigned char* Vp = (const unsigned char*)a.V + (int64_t)it.m * page * (D * 2);
+  const unsigned char* Kp = (const unsigned char*)K + (int64_t)it.m * page * (D * 2);
+  const unsigned char* Vp = (const unsigned char*)V + (int64_t)it.m * page * (D * 2);
   auto scalar_ptr = [](const unsigned char* p) -> void* {
     const uint64_t x = (uint64_t)p;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), up = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));    // (the builtin is signed)
     return (void*)(((uint64_t)up << 32) | lo);
   };
-  // Page numbers of the tile that is loaded next.  Where a page holds whole tiles there is one, and one descriptor for all loads; else one for
-  // each load instruction.  (The second form takes some 150 scalar instructions a tile, which outlast A's S block: a 4096-token chunk on 16384
-  // units, pages of 64, 1000 us instead of 800.)
-  const bool one_page = page >= KT;
-  int ids[4];
-  auto load_ids = [&](int t) __attribute__((always_inline)) {
-    const int tu = __builtin_amdgcn_readfirstlane(t);
-    const int kb = tile_key(tu), end = tu >= t_hi ? 0 : tu < ks_.ns_t ? ks_.ns : ks_.n_keys;
-    if (one_page) {
-      ids[0] = -1;
-      if (kb < end) ids[0] = trow_s[kb >> shift];
-      return;
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int key = kb + (w4 + u * 4) * KPI;
-      ids[u] = -1;
-      if (key < end) ids[u] = trow_s[key >> shift];
-    }
+  // Descriptors: one a tile where a page holds whole tiles (EPT = 1), else one for each of the wavefront's four load instructions.  Their parts are
+  // formed by the lanes of the wavefront, a descriptor each, for 64 / EPT tiles at a time, and read from there; the page numbers of the next
+  // lot are requested with each.  (A 4096-token chunk on 16384 units, pages of 64: formed tile by tile, 120 scalar instructions for four
+  // descriptors 1000 us, one descriptor 911 us, its page number from LDS 909 us.)
+  constexpr int EPT = ONE_PAGE ? 1 : 4, TPL = 64 / EPT;
+  uint32_t e_off = 0, e_up = 0;                                  // this lane's descriptor: offset in the pool ...
+  int e_len = 0, e_id = 0;                                       // ... and bytes there; page number of the next lot's
+  auto entry_key = [&](int i, int& end) __attribute__((always_inline)) {      // first key of this lane's descriptor, lot from tile i of the part
+    const int t = t_lo + i + lane / EPT;
+    end = tile_end(t);
+    return tile_key(t) + (EPT == 1 ? 0 : (w4 + lane % EPT * 4) * KPI);
   };
-  auto issue = [&](int t, int stage) __attribute__((always_inline)) {
-    const int tu = __builtin_amdgcn_readfirstlane(t);
-    const int kb = tile_key(tu), end = tu >= t_hi ? 0 : tu < ks_.ns_t ? ks_.ns : ks_.n_keys;
-    unsigned char* sb = ring + stage * PF_STAGE_B + w4 * 1024;
-    if (one_page) {
-      const uint32_t id = __builtin_amdgcn_readfirstlane(ids[0]);
-      const bool ok = id < (uint32_t)Dm.n_pages;
-      const int len = __builtin_amdgcn_readfirstlane(ok ? min(max(end - kb, 0), KT) * (D * 2) : 0);
-      const uint64_t off = (uint64_t)(ok ? id : 0u) * page_b + (uint32_t)((kb & (page - 1)) * (D * 2));
-      __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Kp + off), 0, len, 0x00020000);
-      __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Vp + off), 0, len, 0x00020000);
-      const int first = w4 * (KPI * D * 2);
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + u * 4096), 16, k_vo, first + u * (4 * KPI * D * 2), 0, 0);
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + u * 4096), 16, v_vo, first + u * (4 * KPI * D * 2), 0, 0);
-      return;
+  auto request = [&](int i) __attribute__((always_inline)) {
+    int end;
+    const int key = entry_key(i, end);
+    e_id = -1;
+    if (key < end) e_id = trow[key >> shift];
+  };
+  auto form = [&](int i) __attribute__((always_inline)) {
+    int end;
+    const int key = entry_key(i, end);
+    const bool ok = (uint32_t)e_id < (uint32_t)Dm.n_pages;
+    const uint64_t off = (uint64_t)(ok ? (uint32_t)e_id : 0u) * page_b + (uint32_t)((key & (page - 1)) * (D * 2));
+    e_off = (uint32_t)off;
+    e_up = (uint32_t)(off >> 32);
+    e_len = ok ? min(max(end - key, 0), EPT == 1 ? KT : KPI) * (D * 2) : 0;
+  };
+  auto issue = [&](int i) __attribute__((always_inline)) {       // tile i of the part, into stage i mod 4
+    const int iu = __builtin_amdgcn_readfirstlane(i);
+    if (iu % TPL == 0) {
+      form(iu);
+      request(iu + TPL);
     }
+    unsigned char* sb = ring + (iu & 3) * PF_STAGE_B + w4 * 1024;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int key = kb + (w4 + u * 4) * KPI;
-      const uint32_t id = __builtin_amdgcn_readfirstlane(ids[u]);
-      const bool ok = id < (uint32_t)Dm.n_pages;
-      const int len = __builtin_amdgcn_readfirstlane(ok ? min(max(end - key, 0), KPI) * (D * 2) : 0);
-      const uint64_t off = (uint64_t)(ok ? id : 0u) * page_b + (uint32_t)((key & (page - 1)) * (D * 2));
+    for (int x = 0; x < EPT; ++x) {
+      const int src = iu % TPL * EPT + x;
+      const uint32_t lo = __builtin_amdgcn_readlane(e_off, src), up = __builtin_amdgcn_readlane(e_up, src);      // (the builtin is signed)
+      const int len = __builtin_amdgcn_readlane(e_len, src);
+      const uint64_t off = ((uint64_t)up << 32) | lo;
       __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Kp + off), 0, len, 0x00020000);
       __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(scalar_ptr(Vp + off), 0, len, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + u * 4096), 16, k_vo, 0, 0, 0);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + u * 4096), 16, v_vo, 0, 0, 0);
+      constexpr int PER = 4 / EPT;                               // load instructions of a descriptor
+      const int first = EPT == 1 ? w4 * (KPI * D * 2) : 0;
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (pf_lds_ptr)(sb + (x + u) * 4096), 16, k_vo, first + u * (4 * KPI * D * 2), 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (pf_lds_ptr)(sb + PF_TILE_B + (x + u) * 4096), 16, v_vo, first + u * (4 * KPI * D * 2), 0, 0);
+      }
     }
   };
 
@@ -318,7 +332,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   auto softmax_pv = [&](f32x16 (&sacc)[NKB], int t, int sb_off) __attribute__((always_inline)) {
     const int kb0 = tile_key(t);
     // does every row of the wavefront see the whole tile?
-    const bool whole = !odd_pages && (t < ks_.ns_t ? kb0 + KT <= ks_.ns : kb0 + KT - 1 <= pw0 && kb0 >= ks_.w_lo && (Dm.window == 0 || pw1 - kb0 < Dm.window));
+    const bool whole = t < ks_.ns_t ? kb0 <= all_sink : kb0 >= all_lo && kb0 <= all_hi;
     if (!whole) {
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
@@ -417,25 +431,19 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   // does some row of the wavefront see some key of tile t?
   auto active = [&](int t) __attribute__((always_inline)) {
     const int kb = tile_key(t);
-    if (!has_rows) return false;
-    if (t < ks_.ns_t) return true;
-    return kb <= pw1 && (Dm.window == 0 || kb + KT - 1 > pw0 - Dm.window || kb < Dm.n_sink);
+    return kb <= any_hi && (t < ks_.ns_t || kb >= any_lo || kb < Dm.n_sink);
   };
   if (wave >= PF_NW / 2) {
-    load_ids(t_lo);
-    issue(t_lo, 0);
-    load_ids(t_lo + 1);
-    issue(t_lo + 1, 1);
-    load_ids(t_lo + 2);
-    issue(t_lo + 2, 2);
-    load_ids(t_lo + 3);
+    request(0);
+    issue(0);
+    issue(1);
+    issue(2);
     asm volatile("s_waitcnt vmcnt(8)" ::: "memory");            // the first two tiles have landed
     wg_barrier();
     for (int t = t_lo; t < t_hi; ++t) {
       const int i = t - t_lo, sb_off = (i & 3) * PF_STAGE_B;
       wg_barrier();                                              // X
-      issue(t + 3, (i + 3) & 3);
-      load_ids(t + 4);
+      issue(i + 3);
       const bool act = active(t);
       if (act) prefetch_k(sb_off);
       wg_barrier();                                              // Y
@@ -468,7 +476,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     // A masked value that is not finite has met the matrix cores.  The wavefront's rows again, key by key: a lane has the dims of its
     // row that its accumulators hold.
     float qv[NDB][16];
-    const bf16_t* qp = (const bf16_t*)a.q + at * D + hi * 4;
+    const bf16_t* qp = q + at * D + hi * 4;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
@@ -542,9 +550,9 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
 template <int D>
 __global__ __launch_bounds__(PF_THREADS) void paged_prefill_join_kernel(PagedAttn a, PagedDims Dm, int n_items, int parts, const float* __restrict__ part) {
   constexpr int NDB = D / 32;
-  extern __shared__ int32_t first[];
+  extern __shared__ __attribute__((aligned(16))) unsigned char scratch[];
   PfItem it;
-  if (!pf_item(a, Dm, blockIdx.x, first, it)) return;
+  if (!pf_item(a, Dm, blockIdx.x, scratch, it)) return;
   const PfKeys k = pf_keys(it, Dm, pf_tile_keys(D));
   const int len = pf_part_len(k.n_tiles, parts), n = (k.n_tiles + len - 1) / len;
   if (n <= 1) return;
@@ -600,9 +608,12 @@ static void prefill_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t st) {
   const int n_items = (int)(tiles * Dm.h_kv);
   int parts = PF_CUS / n_items;
   parts = parts < 1 ? 1 : parts > PF_MAX_PARTS ? PF_MAX_PARTS : parts;
-  paged_prefill_kernel<D><<<(unsigned)n_items * (unsigned)parts, PF_THREADS, 0, st>>>(a, a.table, Dm, n_items, parts, (float*)a.ws);
+  const unsigned n_wg = (unsigned)n_items * (unsigned)parts;
+  const bf16_t *q = (const bf16_t*)a.q, *K = (const bf16_t*)a.K, *V = (const bf16_t*)a.V;
+  if (1 << Dm.page_shift >= pf_tile_keys(D)) paged_prefill_kernel<D, true><<<n_wg, PF_THREADS, 0, st>>>(a, q, K, V, a.table, Dm, n_items, parts, (float*)a.ws);
+  else paged_prefill_kernel<D, false><<<n_wg, PF_THREADS, 0, st>>>(a, q, K, V, a.table, Dm, n_items, parts, (float*)a.ws);
   if (parts > 1)
-    paged_prefill_join_kernel<D><<<dim3((unsigned)n_items, D / 32), PF_THREADS, (size_t)(a.n_req + 1) * sizeof(int32_t), st>>>(a, Dm, n_items, parts, (const float*)a.ws);
+    paged_prefill_join_kernel<D><<<dim3((unsigned)n_items, D / 32), PF_THREADS, PF_SCRATCH + (size_t)(a.n_req + 1) * sizeof(int32_t), st>>>(a, Dm, n_items, parts, (const float*)a.ws);
 }
 
 void launch_paged_prefill(const PagedDims& D, const PagedAttn& a, hipStream_t st) {

@@ -448,6 +448,23 @@ def test_lengths_are_taken_within_the_row():
     close(lse, wl, ltol, "lse")
 
 
+def test_a_chunk_of_many_rows_on_a_long_cache_of_small_pages():
+    """More page numbers than a workgroup keeps at hand (4096), and no parts; sampled rows."""
+    rng = np.random.default_rng(77)
+    n, new = 70001, 4400
+    c = paged_case(rng, "bf16", 8, 8, 32, 16, [n])
+    q, q64 = numbers(rng, "bf16", new, 8, 32)
+    out, lse = run_prefill(c, q, [0, new])
+    rows = [0, 1, 63, 255, 256, 2047, 4350, 4399]
+    KV = [[units(c, c[x], 0, m)[0] for m in range(8)] for x in ("K64", "V64")]
+    for t in rows:
+        see = R.visible(n - new + t, n, 0, 0)
+        for j in range(8):
+            want, wl, tol, ltol = R.attend(q64[t, j], KV[0][j], KV[1][j], see, c["scale"], "bf16")
+            close(out[t, j], want, tol, f"row {t} head {j}")
+            assert abs(lse[t, j] - wl) <= ltol
+
+
 def test_units_behind_four_gigabytes_of_the_pool():
     """Pages whose offset passes 32 bits."""
     page, h_kv, d = 256, 8, 128
