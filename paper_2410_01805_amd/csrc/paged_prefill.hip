@@ -163,8 +163,8 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
 
   auto tile_key = [&](int t) __attribute__((always_inline)) { return t < ks_.ns_t ? t * KT : ks_.wb + (t - ks_.ns_t) * KT; };
   auto tile_end = [&](int t) __attribute__((always_inline)) { return t >= t_hi ? 0 : t < ks_.ns_t ? ks_.ns : ks_.n_keys; };
-  // pages that are not the pool's, among those of the item's keys
-  bool odd_pages;
+  // does a page of the item's keys lie outside the pool?  All rows are then formed key by key.
+  bool redo;                                   // the wavefront's rows have to be formed key by key
   {
     int odd = 0;
     const int s_end = (ks_.ns + page - 1) >> shift, e0 = ks_.wb >> shift, e1 = (ks_.n_keys + page - 1) >> shift;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     __syncthreads();
     if (odd) *said = 1;
     __syncthreads();
-    odd_pages = __builtin_amdgcn_readfirstlane(*said) != 0;
+    redo = __builtin_amdgcn_readfirstlane(*said) != 0;
     __syncthreads();
   }
 
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const int pos = it.p0 + tok;
   const int pw0 = it.p0 + min(wave * 32, rows - 1) / g, pw1 = it.p0 + min(wave * 32 + 31, rows - 1) / g;
   // first keys of the tiles that all rows of the wavefront see whole (among the sinks: up to all_sink), and of those that some row sees a key of
-  const int all_lo = Dm.window ? max(ks_.w_lo, pw1 - Dm.window + 1) : 0, all_hi = odd_pages ? -1 : pw0 - KT + 1, all_sink = odd_pages ? -1 : ks_.ns - KT;
+  const int all_lo = Dm.window ? max(ks_.w_lo, pw1 - Dm.window + 1) : 0, all_hi = pw0 - KT + 1, all_sink = ks_.ns - KT;
   const int any_lo = Dm.window ? pw0 - Dm.window - KT + 2 : 0, any_hi = wave * 32 < rows ? pw1 : -1;
 
   bf16x8 qf[NKS];
@@ -206,7 +206,6 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const float c = Dm.scale * 1.4426950408889634f;
   float m_run = 0.f, l_run = 0.f;              // of the lane's row, in log2 units; the sum over this lane's keys
   bool unset = true;                           // the row has seen no key yet
-  bool redo = false;                           // the wavefront's rows have to be formed key by key
 
   // ---- tiles -----------------------------------------------------------------------------------------------------------
   const int w4 = wave & 3, l_row = lane >> 4, l_pos = lane & 15;
@@ -324,7 +323,6 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     bool s;
     if (t < ks_.ns_t) s = key < ks_.ns && key <= pos;
     else s = key >= ks_.w_lo && key <= pos && (Dm.window == 0 || pos - key < Dm.window || key < Dm.n_sink);
-    if (odd_pages && s) s = (unsigned)trow[key >> shift] < (unsigned)Dm.n_pages;
     return s;
   };
 
@@ -473,7 +471,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // trailing empty loads
 
   if (redo) {
-    // A masked value that is not finite has met the matrix cores.  The wavefront's rows again, key by key: a lane has the dims of its
+    // A masked value that is not finite has met the matrix cores, or a page is not the pool's.  The wavefront's rows again, key by key: a lane has the dims of its
     // row that its accumulators hold.
     float qv[NDB][16];
     const bf16_t* qp = q + at * D + hi * 4;
