@@ -65,11 +65,12 @@ struct PagedAttn {
   float* lse;       // or NULL
   void* ws;
 };
-void launch_paged_attn_simple(const PagedDims& D, const PagedAttn& a, hipStream_t st);
 void launch_paged_decode(const PagedDims& D, const PagedAttn& a, hipStream_t st);
 size_t paged_decode_workspace(const PagedDims& D, int max_reqs);
 void launch_paged_prefill(const PagedDims& D, const PagedAttn& a, hipStream_t st);      // bf16
 size_t paged_prefill_workspace(const PagedDims& D);
+void launch_paged_prefill_f32(const PagedDims& D, const PagedAttn& a, hipStream_t st);
+size_t paged_prefill_f32_workspace(const PagedDims& D);
 
 // A length as the kernels take it.
 __device__ __forceinline__ int paged_len(const int32_t* lens, int r, int max_pages, int page_shift) {

@@ -41,7 +41,7 @@ int validate(const locret_paged_config* c, PagedDims* D) {
 }
 
 size_t workspace_bytes(const PagedDims& D, int max_reqs) {
-  const size_t a = paged_decode_workspace(D, max_reqs), b = paged_prefill_workspace(D);
+  const size_t a = paged_decode_workspace(D, max_reqs), b = D.bf16 ? paged_prefill_workspace(D) : paged_prefill_f32_workspace(D);
   return a > b ? a : b;
 }
 
@@ -60,7 +60,7 @@ int attention(const locret_paged_config* cfg, const PagedAttn& a, size_t bytes, 
     return LOCRET_EALIGN;
   if (bytes < workspace_bytes(D, cfg->max_reqs)) return LOCRET_ENOMEM;
   if (prefill && D.bf16) launch_paged_prefill(D, a, st);
-  else if (prefill) launch_paged_attn_simple(D, a, st);
+  else if (prefill) launch_paged_prefill_f32(D, a, st);
   else launch_paged_decode(D, a, st);
   return launched();
 }

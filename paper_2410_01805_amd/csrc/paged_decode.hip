@@ -10,14 +10,14 @@
 // workgroup leaves maximum, sum and sum of values (two such pieces a workgroup at most), and the second launch, which has a workgroup
 // per request and head, joins them in the order of the keys.  Results depend on no order of execution.
 //
-// Tiles go from memory to registers in the layout of the operands (DecTile for bf16; PagedTileF32, whose products are exact to 32 bits):
+// Tiles go from memory to registers in the layout of the operands (paged_tile.h; float products are those of 32 bits):
 // S^T = K Q^T has keys as rows, in an order in which a lane's accumulators are the eight keys whose probabilities it gives to
 // O = P V.  The next keys are requested as soon as the logits are formed, the next values after their product, page numbers a unit
 // earlier.  Probabilities of bf16 layers become bf16 factors (half a step of 2^-8 each, as large as the rounding of the output, and
 // independent of each other, so less than that in a sum); maximum, sum and accumulators are 32-bit.  The maximum moves only when a logit
 // exceeds it by 8 binary orders.  What is not seen is taken out by selection: its logit before the maximum, its value before the product.
-#include "decode_tile.h"
 #include "paged.h"
+#include "paged_tile.h"
 
 namespace locret {
 
@@ -27,99 +27,6 @@ constexpr float PD_RESCALE_LOG2 = 8.f;
 // Workgroups a CU: what registers allow without spilling.
 template <typename T, int D> struct PagedOcc { static constexpr int value = sizeof(T) == 2 ? (D >= 96 ? 3 : 4) : (D >= 96 ? 2 : 3); };
 static int paged_decode_workgroups(const PagedDims& D) { return 256 * (D.bf16 ? (D.d >= 96 ? 3 : 4) : (D.d >= 96 ? 2 : 3)); }
-
-// DecTile's operands from two places: rows 0..15 and 16..31 of the tile (pages of 16 units; the same place for larger ones).
-template <int D> struct PagedTileBf16 : DecTile<D> {
-  typedef DecTile<D> Base;
-  static constexpr int NQ = Base::NKS;
-  typedef bf16x8 q_t;
-  __device__ __forceinline__ void load_k(const bf16_t* lo, const bf16_t* hi) {
-    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const bf16_t* base = (n >= 8 ? hi : lo) + (8 * (n >> 2) + (n & 3)) * D + kg * 8;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int ks = 0; ks < Base::NKS; ++ks) this->ka[b][ks] = *(const bf16x8*)(base + 4 * b * D + ks * 32);
-  }
-  __device__ __forceinline__ void load_v(const bf16_t* lo, const bf16_t* hi) {
-    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const bf16_t* base = (kg >= 2 ? hi : lo) + 8 * kg * D + n * Base::NV;
-#pragma unroll
-    for (int r = 0; r < 8; ++r) load_words<Base::NV / 2>(base + r * D, this->vw[r]);
-  }
-  __device__ __forceinline__ void clear_v(uint32_t seen) {          // bit r: the lane's key r
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-      for (int w = 0; w < Base::NV / 2; ++w) this->vw[r][w] = (seen >> r) & 1 ? this->vw[r][w] : 0u;
-  }
-  static __device__ __forceinline__ void load_q(const bf16_t* row, bool has, q_t (&qb)[NQ]) {
-    const int kg = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int ks = 0; ks < NQ; ++ks) qb[ks] = has ? *(const bf16x8*)(row + ks * 32 + kg * 8) : bf16x8{};
-  }
-  __device__ __forceinline__ void add(const float (&p)[8], dec_f32x4 (&o)[Base::NV]) const {
-    const uint4 pk = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7]));
-    this->accumulate(__builtin_bit_cast(bf16x8, pk), o);
-  }
-};
-
-// The same for float: v_mfma_f32_16x16x4_f32.  Contraction step (ks, e) of S^T has dim 16 ks + 4 kg + e in lane group kg, so that a lane
-// reads 16 bytes; step r of a block's O = P V has key 4 kg + r there, which is where that key's probability is.
-template <int D> struct PagedTileF32 {
-  static constexpr int NQ = D / 16, NV = D / 16;
-  typedef float4 q_t;
-  float4 ka[2][NQ];
-  float vw[8][NV];
-  __device__ __forceinline__ void load_k(const float* lo, const float* hi) {
-    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const float* base = (n >= 8 ? hi : lo) + (8 * (n >> 2) + (n & 3)) * D + kg * 4;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int ks = 0; ks < NQ; ++ks) ka[b][ks] = *(const float4*)(base + 4 * b * D + ks * 16);
-  }
-  __device__ __forceinline__ void load_v(const float* lo, const float* hi) {
-    const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const float* base = (kg >= 2 ? hi : lo) + 8 * kg * D + n * NV;
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-      for (int i = 0; i < NV; i += 2) *(float2*)&vw[r][i] = *(const float2*)(base + r * D + i);
-  }
-  __device__ __forceinline__ void clear_v(uint32_t seen) {
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-      for (int i = 0; i < NV; ++i) vw[r][i] = (seen >> r) & 1 ? vw[r][i] : 0.f;
-  }
-  static __device__ __forceinline__ void load_q(const float* row, bool has, q_t (&qb)[NQ]) {
-    const int kg = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int ks = 0; ks < NQ; ++ks) qb[ks] = has ? *(const float4*)(row + ks * 16 + kg * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  __device__ __forceinline__ void logits(const q_t (&qb)[NQ], dec_f32x4 (&s)[2]) const {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      s[b] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < NQ; ++ks) {
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].x, qb[ks].x, s[b], 0, 0, 0);
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].y, qb[ks].y, s[b], 0, 0, 0);
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].z, qb[ks].z, s[b], 0, 0, 0);
-        s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(ka[b][ks].w, qb[ks].w, s[b], 0, 0, 0);
-      }
-    }
-  }
-  __device__ __forceinline__ void add(const float (&p)[8], dec_f32x4 (&o)[NV]) const {
-#pragma unroll
-    for (int r = 0; r < 8; ++r)
-#pragma unroll
-      for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[r], vw[r][i], o[i], 0, 0, 0);
-  }
-};
-template <typename T, int D> struct PagedTileOf { typedef PagedTileBf16<D> type; };
-template <int D> struct PagedTileOf<float, D> { typedef PagedTileF32<D> type; };
 
 // The visible units of a request: its sinks, then from the first 32 keys with one in the window on.
 struct PagedSpan {

@@ -605,7 +605,7 @@ __global__ __launch_bounds__(PF_THREADS) void paged_prefill_join_kernel(PagedAtt
   if (a.lse && hi == 0 && db == 0) a.lse[at] = den == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(den)) * 0.6931471805599453f;
 }
 
-size_t paged_prefill_workspace(const PagedDims& D) { return D.bf16 ? (size_t)PF_MAX_SLOTS * PF_ROWS * (D.d + 2) * sizeof(float) : 0; }
+size_t paged_prefill_workspace(const PagedDims& D) { return (size_t)PF_MAX_SLOTS * PF_ROWS * (D.d + 2) * sizeof(float); }
 
 template <int D>
 static void prefill_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t st) {
