@@ -274,33 +274,51 @@ def locret_destroy(ctx) -> None:
 
 
 # ---- many requests on one pool of pages ------------------------------------------------------------------------------
-# Tensors are checked against the configuration (type, density, size: LOCRET_EINVAL, LOCRET_ESHAPE), and the calls go to the device that
-# holds them, on that device's current stream unless one is given.  Addresses (ints) pass through unchecked.
-def _paged_tensor(where, t, dtype, numel, dense=True):
-    if t is None or isinstance(t, int):
-        return
-    if t.dtype != dtype or not t.is_cuda or (dense and not t.is_contiguous()):
+# Tensors are checked against the configuration (type, density, device: LOCRET_EINVAL; size: LOCRET_ESHAPE), and the calls go to the device that
+# holds them, on that device's current stream unless one is given.  Addresses (ints) pass through unchecked.  These calls take a few
+# microseconds on the GPU, so they are written out plainly: some 6 us of host time a call, 15 with a helper per check and a device context.
+_PAGED_DTYPE = {LOCRET_F32: torch.float32, LOCRET_BF16: torch.bfloat16}
+
+
+def _paged_ptr(where, dev, t, dtype, numel):
+    """Address of a dense tensor of at least `numel` elements on device `dev` (None -> NULL; ints pass through)."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
         raise LocretError(LOCRET_EINVAL, where)
     if t.numel() < numel:
         raise LocretError(LOCRET_ESHAPE, where)
+    return t.data_ptr()
 
 
-def _paged_call(where, fn, tensors, stream, *args):
-    devices = {t.device for t in tensors if t is not None and not isinstance(t, int)}
-    if len(devices) > 1:
-        raise LocretError(LOCRET_EINVAL, where)
-    with torch.cuda.device(devices.pop() if devices else None):
-        _check(fn(*args, _stream(stream)), where)
+def _paged_device(where, *tensors) -> int:
+    """Index of the device of the first tensor; -1 (the current device) if all are addresses."""
+    for t in tensors:
+        if t is not None and t.__class__ is not int:
+            dev = t.get_device()
+            if dev < 0:
+                raise LocretError(LOCRET_EINVAL, where)
+            return dev
+    return -1
 
 
-def _paged_dtype(cfg):
-    return torch.bfloat16 if cfg.dtype == LOCRET_BF16 else torch.float32
+# The current stream's handle without a Stream object, where torch offers it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _paged_pool(where, cfg, K, V):
-    n = cfg.n_pages * cfg.n_kv_heads * cfg.page_size * cfg.head_dim
-    _paged_tensor(where, K, _paged_dtype(cfg), n)
-    _paged_tensor(where, V, _paged_dtype(cfg), n)
+def _paged_call(where, fn, dev, args, stream) -> None:
+    current = torch.cuda.current_device()
+    if dev < 0 or dev == current:
+        if stream is None:
+            stream = _raw_stream(current)
+        elif stream.__class__ is not int:
+            stream = stream.cuda_stream
+        rc = fn(*args, stream or None)
+        if rc:
+            raise LocretError(rc, where)
+    else:
+        with torch.cuda.device(dev):
+            _paged_call(where, fn, -1, args, stream)
 
 
 def locret_paged_workspace_bytes(cfg: locret_paged_config) -> int:
@@ -309,12 +327,14 @@ def locret_paged_workspace_bytes(cfg: locret_paged_config) -> int:
 
 def locret_paged_plan(cfg, n_req, lens, n_new, lens_out, block_table, free_pages, n_free, n_free_out, max_tokens, cu_new, slots, positions,
                       stream=None) -> None:
-    where = "locret_paged_plan"
-    for t, n in ((lens, n_req), (n_new, n_req), (lens_out, n_req), (block_table, n_req * cfg.max_pages), (free_pages, cfg.n_pages), (n_free, 1),
-                 (n_free_out, 1), (cu_new, n_req + 1), (slots, max_tokens), (positions, max_tokens)):
-        _paged_tensor(where, t, torch.int32, n)
-    arrays = (lens, n_new, lens_out, block_table, free_pages, n_free, n_free_out, cu_new, slots, positions)
-    _paged_call(where, lib.locret_paged_plan, arrays, stream, C.byref(cfg), n_req, *map(_ptr, arrays[:7]), max_tokens, *map(_ptr, arrays[7:]))
+    w, i32 = "locret_paged_plan", torch.int32
+    dev = _paged_device(w, cu_new, free_pages)
+    args = (C.byref(cfg), n_req, _paged_ptr(w, dev, lens, i32, n_req), _paged_ptr(w, dev, n_new, i32, n_req),
+            _paged_ptr(w, dev, lens_out, i32, n_req), _paged_ptr(w, dev, block_table, i32, n_req * cfg.max_pages),
+            _paged_ptr(w, dev, free_pages, i32, cfg.n_pages), _paged_ptr(w, dev, n_free, i32, 1), _paged_ptr(w, dev, n_free_out, i32, 1),
+            max_tokens, _paged_ptr(w, dev, cu_new, i32, n_req + 1), _paged_ptr(w, dev, slots, i32, max_tokens),
+            _paged_ptr(w, dev, positions, i32, max_tokens))
+    _paged_call(w, lib.locret_paged_plan, dev, args, stream)
 
 
 def locret_rope_frequencies(rotary_dim, theta, scaling=LOCRET_ROPE_PLAIN, factor=1.0, original=0.0, low=0.0, high=0.0, factors=None):
@@ -329,60 +349,65 @@ def locret_rope_frequencies(rotary_dim, theta, scaling=LOCRET_ROPE_PLAIN, factor
     return list(freq), amplitude.value
 
 
+def _paged_rows(where, dev, t, dtype, T, heads, d, st, i):
+    """Address of q, k or v [T][heads][d] with any strides between tokens and heads, which go to st[i], st[i + 1]."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise LocretError(LOCRET_EINVAL, where)
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < T or shape[1] != heads or shape[2] != d or t.stride(2) != 1:
+        raise LocretError(LOCRET_ESHAPE, where)
+    st[i], st[i + 1] = t.stride(0), t.stride(1)
+    return t.data_ptr()
+
+
 def locret_paged_append(cfg, T, q, k, v, positions, slots, freq, rotary_dim, interleaved, amplitude, q_weight, k_weight, eps, q_out, K, V,
                         stream=None, strides=None) -> None:
     """q, k, v: [T][heads][head_dim] with any strides between tokens and heads (`strides` for addresses, see include/locret.h)."""
-    where = "locret_paged_append"
+    w, f32 = "locret_paged_append", torch.float32
     h, m, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
-    st = list(strides) if strides is not None else [h * d, d, m * d, d, m * d, d]
-    if len(st) != 6:
-        raise LocretError(LOCRET_EINVAL, where)
-    for i, (t, heads) in enumerate(((q, h), (k, m), (v, m))):
-        if t is None or isinstance(t, int):
-            continue
-        _paged_tensor(where, t, _paged_dtype(cfg), T * heads * d, dense=False)
-        if t.dim() != 3 or t.shape[0] < T or t.shape[1:] != (heads, d) or t.stride(2) != 1:
-            raise LocretError(LOCRET_ESHAPE, where)
-        st[2 * i: 2 * i + 2] = [t.stride(0), t.stride(1)] if strides is None else st[2 * i: 2 * i + 2]
-    _paged_tensor(where, q_out, _paged_dtype(cfg), T * h * d)
-    _paged_tensor(where, positions, torch.int32, T)
-    _paged_tensor(where, slots, torch.int32, T)
-    _paged_tensor(where, freq, torch.float64, rotary_dim // 2)
-    _paged_tensor(where, q_weight, torch.float32, d)
-    _paged_tensor(where, k_weight, torch.float32, d)
-    _paged_pool(where, cfg, K, V)
-    addr = lambda t: t.data_ptr() if torch.is_tensor(t) else t
-    _paged_call(where, lib.locret_paged_append, (q, k, v, positions, slots, freq, q_weight, k_weight, q_out, K, V), stream, C.byref(cfg), T, addr(q),
-                addr(k), addr(v), (C.c_int64 * 6)(*st), addr(positions), addr(slots), addr(freq), rotary_dim, 1 if interleaved else 0,
-                amplitude, addr(q_weight), addr(k_weight), eps, addr(q_out), addr(K), addr(V))
-
-
-def _paged_attention(where, cfg, n_req, T, q, K, V, block_table, lens, cu_new, out, lse, workspace):
-    n = T * cfg.n_q_heads
-    _paged_tensor(where, q, _paged_dtype(cfg), n * cfg.head_dim)
-    _paged_tensor(where, out, _paged_dtype(cfg), n * cfg.head_dim)
-    _paged_tensor(where, lse, torch.float32, n)
-    _paged_tensor(where, block_table, torch.int32, n_req * cfg.max_pages)
-    _paged_tensor(where, lens, torch.int32, n_req)
-    _paged_tensor(where, cu_new, torch.int32, n_req + 1)
-    _paged_pool(where, cfg, K, V)
-    return workspace.numel() * workspace.element_size() if torch.is_tensor(workspace) else 0
+    pool, dtype = cfg.n_pages * m * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
+    dev = _paged_device(w, q, K)
+    if strides is None:
+        st = (C.c_int64 * 6)(h * d, d, m * d, d, m * d, d)
+    elif len(strides) == 6:
+        st = (C.c_int64 * 6)(*strides)
+    else:
+        raise LocretError(LOCRET_EINVAL, w)
+    args = (C.byref(cfg), T, _paged_rows(w, dev, q, dtype, T, h, d, st, 0), _paged_rows(w, dev, k, dtype, T, m, d, st, 2),
+            _paged_rows(w, dev, v, dtype, T, m, d, st, 4), st, _paged_ptr(w, dev, positions, torch.int32, T),
+            _paged_ptr(w, dev, slots, torch.int32, T), _paged_ptr(w, dev, freq, torch.float64, rotary_dim // 2), rotary_dim,
+            1 if interleaved else 0, amplitude, _paged_ptr(w, dev, q_weight, f32, d), _paged_ptr(w, dev, k_weight, f32, d), eps,
+            _paged_ptr(w, dev, q_out, dtype, T * h * d), _paged_ptr(w, dev, K, dtype, pool), _paged_ptr(w, dev, V, dtype, pool))
+    _paged_call(w, lib.locret_paged_append, dev, args, stream)
 
 
 def locret_paged_decode(cfg, n_req, q, K, V, block_table, lens, out, lse, workspace, stream=None, workspace_bytes=None) -> None:
-    where = "locret_paged_decode"
-    have = _paged_attention(where, cfg, n_req, n_req, q, K, V, block_table, lens, None, out, lse, workspace)
-    arrays = (q, K, V, block_table, lens, out, lse, workspace)
-    _paged_call(where, lib.locret_paged_decode, arrays, stream, C.byref(cfg), n_req, *map(_ptr, arrays),
-                have if workspace_bytes is None else workspace_bytes)
+    w, i32 = "locret_paged_decode", torch.int32
+    h, d = cfg.n_q_heads, cfg.head_dim
+    n, pool, dtype = n_req * h * d, cfg.n_pages * cfg.n_kv_heads * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
+    dev = _paged_device(w, q, K, block_table)
+    if workspace_bytes is None:
+        workspace_bytes = workspace.nbytes if torch.is_tensor(workspace) else 0
+    args = (C.byref(cfg), n_req, _paged_ptr(w, dev, q, dtype, n), _paged_ptr(w, dev, K, dtype, pool), _paged_ptr(w, dev, V, dtype, pool),
+            _paged_ptr(w, dev, block_table, i32, n_req * cfg.max_pages), _paged_ptr(w, dev, lens, i32, n_req), _paged_ptr(w, dev, out, dtype, n),
+            _paged_ptr(w, dev, lse, torch.float32, n_req * h), _paged_ptr(w, dev, workspace, torch.uint8, 0), workspace_bytes)
+    _paged_call(w, lib.locret_paged_decode, dev, args, stream)
 
 
 def locret_paged_prefill(cfg, n_req, T, q, K, V, block_table, lens, cu_new, out, lse, workspace, stream=None, workspace_bytes=None) -> None:
-    where = "locret_paged_prefill"
-    have = _paged_attention(where, cfg, n_req, T, q, K, V, block_table, lens, cu_new, out, lse, workspace)
-    arrays = (q, K, V, block_table, lens, cu_new, out, lse, workspace)
-    _paged_call(where, lib.locret_paged_prefill, arrays, stream, C.byref(cfg), n_req, T, *map(_ptr, arrays),
-                have if workspace_bytes is None else workspace_bytes)
+    w, i32 = "locret_paged_prefill", torch.int32
+    h, d = cfg.n_q_heads, cfg.head_dim
+    n, pool, dtype = T * h * d, cfg.n_pages * cfg.n_kv_heads * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
+    dev = _paged_device(w, q, K, block_table)
+    if workspace_bytes is None:
+        workspace_bytes = workspace.nbytes if torch.is_tensor(workspace) else 0
+    args = (C.byref(cfg), n_req, T, _paged_ptr(w, dev, q, dtype, n), _paged_ptr(w, dev, K, dtype, pool), _paged_ptr(w, dev, V, dtype, pool),
+            _paged_ptr(w, dev, block_table, i32, n_req * cfg.max_pages), _paged_ptr(w, dev, lens, i32, n_req),
+            _paged_ptr(w, dev, cu_new, i32, n_req + 1), _paged_ptr(w, dev, out, dtype, n), _paged_ptr(w, dev, lse, torch.float32, T * h),
+            _paged_ptr(w, dev, workspace, torch.uint8, 0), workspace_bytes)
+    _paged_call(w, lib.locret_paged_prefill, dev, args, stream)
 
 
 # ---- convenience: config from a synth.Workload, a context that owns its workspace tensor -----------------
@@ -509,7 +534,7 @@ class PagedCache:
         nbytes = locret_paged_workspace_bytes(cfg)
         if nbytes == 0:
             raise LocretError(LOCRET_EINVAL, "locret_paged_workspace_bytes")
-        self.tdtype = _paged_dtype(cfg)
+        self.tdtype = _PAGED_DTYPE[cfg.dtype]
         ints = dict(dtype=torch.int32, device=self.device)
         pool = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
         self.K, self.V = torch.empty(pool, dtype=self.tdtype, device=self.device), torch.empty(pool, dtype=self.tdtype, device=self.device)

@@ -72,36 +72,68 @@ size_t paged_prefill_workspace(const PagedDims& D);
 void launch_paged_prefill_f32(const PagedDims& D, const PagedAttn& a, hipStream_t st);
 size_t paged_prefill_f32_workspace(const PagedDims& D);
 
+// Data that a launch only reads, from places that are the same in a wavefront: through the scalar cache.
+typedef const __attribute__((address_space(4))) int32_t* paged_const_i32;
+
 // A length as the kernels take it.
 __device__ __forceinline__ int paged_len(const int32_t* lens, int r, int max_pages, int page_shift) {
   return min(max(lens[r], 0), max_pages << page_shift);
 }
 
-__device__ __forceinline__ int64_t shfl_up64(int64_t x, int by) {
-  const int lo = __shfl_up((int)(uint32_t)x, by, 64), hi = __shfl_up((int)(x >> 32), by, 64);
-  return (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+
+// Inclusive sums over the lanes of a wavefront: within rows of 16 lanes by shifts, then the last lane of each row on to the next ones.
+__device__ __forceinline__ uint32_t wave_inclusive(uint32_t x) {
+  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));      // row_shr:1, 2, 4, 8
+  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));      // row_bcast:15 into rows 1 and 3
+  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));      // row_bcast:31 into rows 2 and 3
+  return x;
+}
+// Exclusive sums of N values over the workgroup's threads, and their totals; sums that pass 32 bits stay at 2^32 - 1.  part: N words a wavefront,
+// free again after the next barrier.
+template <int N> __device__ __forceinline__ void block_exclusive(const uint32_t (&x)[N], uint32_t (&before)[N], uint32_t (&total)[N], uint32_t* part) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  uint32_t s[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    s[i] = wave_inclusive(x[i]);
+    if (lane == 63) part[wave * N + i] = s[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) before[i] = total[i] = 0;
+  for (int w = 0; w < nw; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t y = part[w * N + i];
+      if (w < wave) before[i] = add_sat(before[i], y);
+      total[i] = add_sat(total[i], y);
+    }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t own = __shfl_up(s[i], 1, 64);                       // inclusive sum of the lane before
+    before[i] = add_sat(before[i], lane ? own : 0u);
+  }
+}
+__device__ __forceinline__ uint32_t block_exclusive(uint32_t x, uint32_t* part, uint32_t& total) {
+  const uint32_t in[1] = {x};
+  uint32_t before[1], all[1];
+  block_exclusive<1>(in, before, all, part);
+  total = all[0];
+  return before[0];
 }
 
-// Exclusive sums of x over the workgroup's threads; `total` gets the sum of all.  part: one entry a wavefront, not in use by others
-// until the next barrier but one.
-__device__ __forceinline__ int64_t block_exclusive(int64_t x, int64_t* part, int64_t& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  int64_t s = x;
-#pragma unroll
-  for (int by = 1; by < 64; by <<= 1) {
-    const int64_t y = shfl_up64(s, by);
-    if (lane >= by) s += y;
+// The last i in 0 .. n - 1 with first[i] <= x (first does not fall, first[0] <= x).
+__device__ __forceinline__ int last_at_or_before(const int32_t* first, int n, int x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= x) lo = mid; else hi = mid - 1;
   }
-  if (lane == 63) part[wave] = s;
-  __syncthreads();
-  int64_t before = 0;
-  total = 0;
-  for (int w = 0; w < nw; ++w) {
-    const int64_t y = part[w];
-    if (w < wave) before += y;
-    total += y;
-  }
-  return before + s - x;
+  return lo;
 }
 
 // An entry of cu_new as the kernels take it.

@@ -43,6 +43,33 @@ __device__ __forceinline__ PagedSpan paged_span(int n, int window, int n_sink) {
   return s;
 }
 
+// Units a workgroup takes.  (Divisions of 64 bits take a microsecond; sums of units that need them are rare.)
+__device__ __forceinline__ int64_t units_per_wg(int64_t all, int n_wg) {
+  if (all < (int64_t)1 << 30) return ((uint32_t)all + n_wg - 1) / (uint32_t)n_wg;
+  return (all + n_wg - 1) / n_wg;
+}
+// The request, item and tile of unit u (below the number of units); the same in the whole wavefront.
+__device__ __forceinline__ void find_unit(const int32_t* first, int n_req, int items, int64_t u, int& r, int& item, int& tile) {
+  int lo = 0, hi = n_req - 1;
+  while (lo < hi) {                                        // the last request that begins at or before u
+    const int mid = (lo + hi + 1) >> 1;
+    if ((int64_t)first[mid] * items <= u) lo = mid; else hi = mid - 1;
+  }
+  const int64_t in = u - (int64_t)first[lo] * items;
+  const int t = first[lo + 1] - first[lo];
+  int i, k;
+  if (in < (int64_t)1 << 31) {
+    i = (int)((uint32_t)in / (uint32_t)t);
+    k = (int)((uint32_t)in - (uint32_t)i * (uint32_t)t);
+  } else {
+    i = (int)(in / t);
+    k = (int)(in % t);
+  }
+  r = __builtin_amdgcn_readfirstlane(lo);
+  item = __builtin_amdgcn_readfirstlane(i);
+  tile = __builtin_amdgcn_readfirstlane(k);
+}
+
 // Where a piece lies in the workspace.
 struct PagedPieces {
   int32_t* first;     // [n_req + 1] units of one head before each request (their sum fits by the configuration's limits)
@@ -61,14 +88,14 @@ size_t paged_decode_workspace(const PagedDims& D, int max_reqs) {
   return (size_t)((char*)paged_pieces(nullptr, max_reqs, n_wg).o - (char*)nullptr) + (size_t)2 * n_wg * rows * D.d * sizeof(float);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool SMALL>
 __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_decode_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm,
                                                                                            int passes, int ipt) {
-  typedef typename PagedTileOf<T, D>::type Tile;
+  typedef typename PagedTileOf<T, D, SMALL>::type Tile;
   constexpr int NV = D / 16;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float2 wml[PD_NW][PD_HEADS];
-  __shared__ int64_t scan[PD_NW];
+  __shared__ uint32_t scan[PD_NW];
   float* sets = (float*)smem;                              // [wavefront][rows][D]
   const int rows_max = min(Dm.g, PD_HEADS);
   int32_t* first = (int32_t*)(smem + (size_t)PD_NW * rows_max * D * sizeof(float));
@@ -76,7 +103,7 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
   const PagedPieces pc = paged_pieces(a.ws, a.n_req, gridDim.x);
 
   // units of one head before every request
-  int64_t mine = 0, total;
+  uint32_t mine = 0, total;
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < a.n_req) {
@@ -85,7 +112,7 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
       mine += t;
     }
   }
-  int64_t before = block_exclusive(mine, scan, total);
+  uint32_t before = block_exclusive(mine, scan, total);
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < a.n_req) {
@@ -100,22 +127,12 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
   }
   __syncthreads();
   const int items = Dm.h_kv * passes;
-  const int64_t all = total * items, per = (all + gridDim.x - 1) / gridDim.x;
+  const int64_t all = (int64_t)total * items, per = units_per_wg(all, gridDim.x);
   int64_t u = per * blockIdx.x;
   const int64_t u_end = min(all, u + per);
   if (u >= u_end) return;
-  int r = 0, item, tile;
-  {
-    int lo = 0, hi = a.n_req - 1;                          // the last request that begins at or before u
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if ((int64_t)first[mid] * items <= u) lo = mid; else hi = mid - 1;
-    }
-    r = __builtin_amdgcn_readfirstlane(lo);
-    const int64_t in = u - (int64_t)first[r] * items, t = first[r + 1] - first[r];
-    item = __builtin_amdgcn_readfirstlane((int)(in / t));
-    tile = __builtin_amdgcn_readfirstlane((int)(in % t));
-  }
+  int r, item, tile;
+  find_unit(first, a.n_req, items, u, r, item, tile);
   const float c = Dm.scale * 1.4426950408889634f;
   const int shift = Dm.page_shift, page = 1 << shift;
   bool begun = false;                                      // this workgroup has left a piece already: the next one goes to the second place
@@ -125,7 +142,7 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
     const int m = item / passes, hp = item % passes;
     const int j0 = m * Dm.g + hp * PD_HEADS, ng = min(PD_HEADS, Dm.g - hp * PD_HEADS);
     const int t_end = (int)min((int64_t)sp.total, tile + (u_end - u));
-    const int32_t* row = table + (int64_t)r * Dm.max_pages;
+    const paged_const_i32 row = (paged_const_i32)(uint64_t)(table + (int64_t)r * Dm.max_pages);
     const T* Kp = (const T*)a.K + (int64_t)m * page * D;
     const T* Vp = (const T*)a.V + (int64_t)m * page * D;
     const int64_t page_stride = (int64_t)Dm.h_kv * page * D;
@@ -141,7 +158,7 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
       p.id0 = p.id1 = -1;
       if (p.kb < p.hi) {
         p.id0 = row[p.kb >> shift];
-        p.id1 = shift == 4 ? (p.kb + 16 < p.hi ? row[(p.kb >> 4) + 1] : -1) : p.id0;
+        p.id1 = SMALL ? (p.kb + 16 < p.hi ? row[(p.kb >> 4) + 1] : -1) : p.id0;
       }
       return p;
     };
@@ -149,7 +166,7 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
       // (a number that is not the pool's: page 0, whose rows are masked then)
       const int i0 = (unsigned)p.id0 < (unsigned)Dm.n_pages ? p.id0 : 0, i1 = (unsigned)p.id1 < (unsigned)Dm.n_pages ? p.id1 : 0;
       lo = base + i0 * page_stride + (p.kb & (page - 1)) * D;
-      hi = shift == 4 ? base + i1 * page_stride - 16 * D : lo;
+      hi = SMALL ? base + i1 * page_stride - 16 * D : lo;
     };
 
     typename Tile::q_t qb[Tile::NQ];
@@ -238,7 +255,9 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
     __syncthreads();
     const bool whole = tile == 0 && t_end == sp.total;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (begun ? 1 : 0);
-    for (int idx = tid; idx < ng * (D / 4); idx += PD_THREADS) {
+    int tid_ = tid;
+    asm volatile("" : "+v"(tid_));                         // (what follows from it is formed here, not kept in registers over the tiles)
+    for (int idx = tid_; idx < ng * (D / 4); idx += PD_THREADS) {
       const int head = idx / (D / 4), e = idx % (D / 4) * 4;
       float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -297,20 +316,17 @@ __global__ __launch_bounds__(PD_THREADS) void paged_decode_join_kernel(PagedAttn
     return;
   }
   const int items = Dm.h_kv * passes, in = j % Dm.g, item = j / Dm.g * passes + in / PD_HEADS, head = in % PD_HEADS, rows_max = min(Dm.g, PD_HEADS);
-  const int64_t per = ((int64_t)pc.first[a.n_req] * items + n_wg - 1) / n_wg, u0 = (int64_t)f0 * items + (int64_t)item * t, u1 = u0 + t;
-  const int w0 = (int)(u0 / per), w1 = (int)((u1 - 1) / per);
+  const int64_t per = units_per_wg((int64_t)pc.first[a.n_req] * items, n_wg), u0 = (int64_t)f0 * items + (int64_t)item * t, u1 = u0 + t;
+  const bool fits = u1 < (int64_t)1 << 31;
+  const int w0 = fits ? (int)((uint32_t)u0 / (uint32_t)per) : (int)(u0 / per), w1 = fits ? (int)((uint32_t)(u1 - 1) / (uint32_t)per) : (int)((u1 - 1) / per);
   if (w0 == w1) return;
-  // the first workgroup's piece: its second place if it had left one before, that is if its first item was cut at its start and ended there
+  // The first workgroup's piece lies in its second place if it had left one before: if its first unit is not the first of an item.
   const int64_t b0 = per * w0;
   bool second = false;
   if (b0 < u0) {
-    // the item that unit b0 belongs to began before b0?
-    int lo = 0, hi = r;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if ((int64_t)pc.first[mid] * items <= b0) lo = mid; else hi = mid - 1;
-    }
-    second = (b0 - (int64_t)pc.first[lo] * items) % (pc.first[lo + 1] - pc.first[lo]) != 0;
+    int br, bi, bt;
+    find_unit(pc.first, r + 1, items, b0, br, bi, bt);
+    second = bt != 0;
   }
   float M = -INFINITY, L = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -363,7 +379,8 @@ static void decode_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t st) {
   const int n_wg = paged_decode_workgroups(Dm), passes = (Dm.g + PD_HEADS - 1) / PD_HEADS;
   const int rows = Dm.g < PD_HEADS ? Dm.g : PD_HEADS, ipt = (a.n_req + PD_THREADS - 1) / PD_THREADS;
   const size_t lds = (size_t)PD_NW * rows * D * sizeof(float) + (size_t)(a.n_req + 1) * sizeof(int32_t);
-  paged_decode_kernel<T, D><<<(unsigned)n_wg, PD_THREADS, lds, st>>>(a, a.table, Dm, passes, ipt);
+  if (Dm.page_shift == 4) paged_decode_kernel<T, D, true><<<(unsigned)n_wg, PD_THREADS, lds, st>>>(a, a.table, Dm, passes, ipt);
+  else paged_decode_kernel<T, D, false><<<(unsigned)n_wg, PD_THREADS, lds, st>>>(a, a.table, Dm, passes, ipt);
   paged_decode_join_kernel<T, D><<<dim3((unsigned)Dm.h, (unsigned)a.n_req), PD_THREADS, 0, st>>>(a, Dm, passes, n_wg);
 }
 

@@ -5,10 +5,10 @@
 //   W_r = sum of the pages wanted before r:               page number held_r + i of request r is free_pages[F - 1 - W_r - i], F = all free
 //   N_r = sum of new tokens before r:                     its token i is token N_r + i, at position len_r + i
 // so everything follows from three prefix sums over at most 4096 requests, which one workgroup forms in registers and LDS
-// (4 requests a thread).  Bound by latency: a step of 48 requests moves a kilobyte.  Up to PLAN_ONE tokens the same workgroup writes
-// tables and slots too; more of them (prompts) are written by a second launch over all CUs, whose workgroups form the sums of W and N again
-// from what the first one left (lens_out and cu_new give the lengths before the step), so that no workspace is needed
-// and the lengths may be updated in place.
+// (4 requests a thread).  Pages and tokens are then dealt out to threads one by one, each finding its request by bisection.  Bound by latency: a
+// step of 48 requests moves a kilobyte.  Up to PLAN_ONE tokens the same workgroup writes tables and slots too; more of them (prompts)
+// are written by a second launch over all CUs, whose workgroups form the sums of W and N again from what the first one left (lens_out and
+// cu_new give the lengths before the step), so that no workspace is needed and the lengths may be updated in place.
 #include "paged.h"
 
 namespace locret {
@@ -21,34 +21,40 @@ struct PlanSmem {
   int len[PAGED_MAX_REQS];          // units before the step (0 where the request is finished)
   int cu[PAGED_MAX_REQS + 1];       // N_r
   int want[PAGED_MAX_REQS + 1];     // W_r
-  int64_t part[3][PLAN_MAX_THREADS / 64];
+  uint32_t part[3 * PLAN_MAX_THREADS / 64];
 };
 
 __device__ __forceinline__ int pages_of(int units, int shift) { return (int)(((int64_t)units + (1 << shift) - 1) >> shift); }
 
-// Table entries of requests r0, r0 + r_step, ... (a wavefront each) and slots of the tokens [t0, t1), from the sums in LDS.
-__device__ __forceinline__ void plan_fill(const PagedPlan& p, const PlanSmem& s, int n_all_free, int r0, int r_step, int t0, int t1) {
-  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 63;
-  const int total = s.cu[p.n_req];
-  for (int r = r0 + (tid >> 6); r < p.n_req; r += r_step) {
-    const int held = pages_of(s.len[r], p.page_shift), n = s.want[r + 1] - s.want[r], top = n_all_free - 1 - s.want[r];
-    for (int i = lane; i < n; i += 64) p.table[(int64_t)r * p.max_pages + held + i] = p.free_pages[top - i];
+// Table entries: pages [i0, n_pages) of the step in steps of i_step; slots of tokens t0 .. t1 - 1, four in a row a thread.
+__device__ __forceinline__ void plan_fill(const PagedPlan& p, const PlanSmem& s, int n_all_free, int i0, int i_step, int t0, int t1) {
+  const int n_new_pages = s.want[p.n_req], total = s.cu[p.n_req];
+#pragma unroll 2
+  for (int i = i0; i < n_new_pages; i += i_step) {
+    const int r = last_at_or_before(s.want, p.n_req, i);
+    p.table[(int64_t)r * p.max_pages + pages_of(s.len[r], p.page_shift) + (i - s.want[r])] = p.free_pages[n_all_free - 1 - i];
   }
-  for (int t = t0 + tid; t < t1; t += nt) {
-    int slot = -1, pos = 0;
-    if (t < total) {
-      int lo = 0, hi = p.n_req - 1;                    // the last request whose first token is at most t
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (s.cu[mid] <= t) lo = mid; else hi = mid - 1;
+  for (int t = t0; t < t1; t += 4 * blockDim.x) {
+    int slot[4], pos[4], r = t < total ? last_at_or_before(s.cu, p.n_req, t) : 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      slot[e] = -1;
+      pos[e] = 0;
+      if (t + e < total) {
+        while (s.cu[r + 1] <= t + e) ++r;
+        pos[e] = s.len[r] + (t + e - s.cu[r]);
+        const int page = pos[e] >> p.page_shift, i = page - pages_of(s.len[r], p.page_shift);
+        const int id = i < 0 ? p.table[(int64_t)r * p.max_pages + page] : p.free_pages[n_all_free - 1 - s.want[r] - i];
+        // (else the table or the list was not the pool's)
+        if (id >= 0 && id < p.n_pages) slot[e] = (id << p.page_shift) | (pos[e] & ((1 << p.page_shift) - 1));
       }
-      pos = s.len[lo] + (t - s.cu[lo]);
-      const int page = pos >> p.page_shift, i = page - pages_of(s.len[lo], p.page_shift);
-      const int id = i < 0 ? p.table[(int64_t)lo * p.max_pages + page] : p.free_pages[n_all_free - 1 - s.want[lo] - i];
-      if (id >= 0 && id < p.n_pages) slot = (id << p.page_shift) | (pos & ((1 << p.page_shift) - 1));      // (else the table or the list was not the pool's)
     }
-    p.slots[t] = slot;
-    p.positions[t] = pos;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (t + e < t1) {
+        p.slots[t + e] = slot[e];
+        p.positions[t + e] = pos[e];
+      }
   }
 }
 
@@ -56,90 +62,97 @@ __global__ __launch_bounds__(PLAN_MAX_THREADS) void plan_kernel(PagedPlan p, int
   __shared__ PlanSmem s;
   const int tid = threadIdx.x, nt = blockDim.x;
   const int most = p.max_pages << p.page_shift;
-  int len[PLAN_IPT], add[PLAN_IPT];                    // add: tokens asked for, -1 finished
-  int64_t back = 0, want = 0, tok = 0;
+  int len[PLAN_IPT], add[PLAN_IPT], held[PLAN_IPT];    // add: tokens asked for, -1 finished
+  uint32_t mine[3] = {0, 0, 0}, before[3], all[3];     // pages given back, pages wanted, tokens
 #pragma unroll
   for (int u = 0; u < PLAN_IPT; ++u) {
     const int r = tid * ipt + u;
-    len[u] = add[u] = 0;
+    len[u] = add[u] = held[u] = 0;
     if (u < ipt && r < p.n_req) {
       len[u] = min(max(p.lens[r], 0), most);
       add[u] = p.n_new[r];
-      if (add[u] < 0) { add[u] = -1; back += pages_of(len[u], p.page_shift); }
+      held[u] = pages_of(len[u], p.page_shift);
+      if (add[u] < 0) { add[u] = -1; mine[0] = add_sat(mine[0], held[u]); }
       else if (add[u] > most - len[u]) add[u] = 0;
       if (add[u] > 0) {
-        want += pages_of(len[u] + add[u], p.page_shift) - pages_of(len[u], p.page_shift);
-        tok += add[u];
+        mine[1] = add_sat(mine[1], pages_of(len[u] + add[u], p.page_shift) - held[u]);
+        mine[2] = add_sat(mine[2], add[u]);
       }
     }
   }
   const int n_free = min(max(p.n_free[0], 0), p.n_pages);
-  int64_t all_back, all_want, all_tok;
-  int64_t b = block_exclusive(back, s.part[0], all_back);
-  int64_t w = block_exclusive(want, s.part[1], all_want);
-  int64_t n = block_exclusive(tok, s.part[2], all_tok);
-  const int n_all_free = (int)(n_free + all_back < p.n_pages ? n_free + all_back : p.n_pages);
-  // what fits, a prefix of the requests: both sums only grow
-  int64_t w_in = 0, n_in = 0;                          // of the served ones of this thread
+  block_exclusive<3>(mine, before, all, s.part);
+  const int n_all_free = (int)min(add_sat(n_free, all[0]), (uint32_t)p.n_pages);
+  if (all[0] > 0) {
+    // pages of finished requests: s.want and s.len hold B_r and the lengths meanwhile
+    uint32_t b = before[0];
+#pragma unroll
+    for (int u = 0; u < PLAN_IPT; ++u) {
+      const int r = tid * ipt + u;
+      if (u < ipt && r < p.n_req) {
+        s.want[r] = (int)min(b, (uint32_t)INT32_MAX);
+        if (add[u] < 0) b = add_sat(b, held[u]);
+      }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < n_all_free - n_free; i += nt) {
+      const int r = last_at_or_before(s.want, p.n_req, i);
+      p.free_pages[n_free + i] = p.table[(int64_t)r * p.max_pages + (i - s.want[r])];
+    }
+    __syncthreads();
+  }
+  // What fits is a prefix of the requests, since both sums only grow.
+  uint32_t served[2] = {0, 0};                         // pages and tokens of this thread's served ones
   bool fits = true;
 #pragma unroll
   for (int u = 0; u < PLAN_IPT; ++u) {
-    const int r = tid * ipt + u;
-    if (u < ipt && r < p.n_req) {
-      const int held = pages_of(len[u], p.page_shift);
-      if (add[u] < 0) {
-        const int32_t* row = p.table + (int64_t)r * p.max_pages;
-        for (int i = 0; i < held; ++i)
-          if (n_free + b + i < p.n_pages) p.free_pages[n_free + b + i] = row[i];
-        b += held;
-        len[u] = 0;
-      }
-      if (add[u] > 0) {
-        const int pages = pages_of(len[u] + add[u], p.page_shift) - held;
-        fits = fits && w + w_in + pages <= n_all_free && n + n_in + add[u] <= p.max_tokens;
-        if (!fits) add[u] = 0;
-        else { w_in += pages; n_in += add[u]; }
-      }
+    if (add[u] < 0) len[u] = held[u] = 0;
+    if (add[u] > 0) {
+      const uint32_t pages = pages_of(len[u] + add[u], p.page_shift) - held[u];
+      fits = fits && add_sat(before[1], served[0] + pages) <= (uint32_t)n_all_free && add_sat(before[2], add_sat(served[1], add[u])) <= (uint32_t)p.max_tokens;
+      if (!fits) add[u] = 0;
+      else { served[0] += pages; served[1] += add[u]; }
     }
   }
-  // Sums over the served ones.  A thread behind the first request that did not fit has served nothing, and its own sums lie
-  // above the limits already, so the sums of all served requests are those of the last thread that served any.
-  __syncthreads();                                     // part[] is free again, free_pages is complete for this workgroup
-  int64_t sum_w, sum_n;
-  const int64_t w0 = block_exclusive(w_in, s.part[0], sum_w), n0 = block_exclusive(n_in, s.part[1], sum_n);
-  int cw = (int)w0, cn = (int)n0;
+  // A thread behind the first request that did not fit has served nothing.
+  uint32_t at[2] = {before[1], before[2]}, sum[2] = {all[1], all[2]};
+  if (all[1] > (uint32_t)n_all_free || all[2] > (uint32_t)p.max_tokens) {      // (the same in the whole workgroup)
+    __syncthreads();                                   // s.part is free again
+    block_exclusive<2>(served, at, sum, s.part);
+  }
 #pragma unroll
   for (int u = 0; u < PLAN_IPT; ++u) {
     const int r = tid * ipt + u;
     if (u < ipt && r < p.n_req) {
       s.len[r] = len[u];
-      s.cu[r] = cn;
-      s.want[r] = cw;
-      p.cu_new[r] = cn;
+      s.want[r] = (int)at[0];
+      s.cu[r] = (int)at[1];
+      p.cu_new[r] = (int)at[1];
       if (add[u] > 0) {
-        cw += pages_of(len[u] + add[u], p.page_shift) - pages_of(len[u], p.page_shift);
-        cn += add[u];
+        at[0] += pages_of(len[u] + add[u], p.page_shift) - held[u];
+        at[1] += add[u];
       }
       p.lens_out[r] = len[u] + max(add[u], 0);
     }
   }
   if (tid == 0) {
-    s.cu[p.n_req] = (int)sum_n;
-    s.want[p.n_req] = (int)sum_w;
-    p.cu_new[p.n_req] = (int)sum_n;
-    p.n_free_out[0] = n_all_free - (int)sum_w;
+    s.want[p.n_req] = (int)sum[0];
+    s.cu[p.n_req] = (int)sum[1];
+    p.cu_new[p.n_req] = (int)sum[1];
+    p.n_free_out[0] = n_all_free - (int)sum[0];
   }
   if (!fill) return;
   __syncthreads();
-  plan_fill(p, s, n_all_free, 0, nt >> 6, 0, p.max_tokens);
+  plan_fill(p, s, n_all_free, tid, nt, 4 * tid, p.max_tokens);
 }
 
-// Tables and slots of a long step: workgroup b takes a share of the tokens and every gridDim.x-th four requests.
+// Tables and slots of a long step: every workgroup takes a share of the tokens and of the pages.
 __global__ __launch_bounds__(FILL_THREADS) void plan_fill_kernel(PagedPlan p) {
   __shared__ PlanSmem s;
   const int tid = threadIdx.x;
   const int ipt = (p.n_req + FILL_THREADS - 1) / FILL_THREADS;
-  int64_t want = 0, all;
+  uint32_t want = 0, all;
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < p.n_req) {
@@ -152,7 +165,7 @@ __global__ __launch_bounds__(FILL_THREADS) void plan_fill_kernel(PagedPlan p) {
       if (r == p.n_req - 1) s.cu[p.n_req] = c1;
     }
   }
-  int64_t before = block_exclusive(want, s.part[0], all);
+  uint32_t before = block_exclusive(want, s.part, all);
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < p.n_req) { const int pages = s.want[r]; s.want[r] = (int)before; before += pages; }
@@ -161,7 +174,7 @@ __global__ __launch_bounds__(FILL_THREADS) void plan_fill_kernel(PagedPlan p) {
   __syncthreads();
   const int n_all_free = p.n_free_out[0] + (int)all;
   const int t0 = blockIdx.x * FILL_TOKENS, left = p.max_tokens - t0;
-  plan_fill(p, s, n_all_free, blockIdx.x * (FILL_THREADS / 64), gridDim.x * (FILL_THREADS / 64), t0, t0 + min(left, FILL_TOKENS));
+  plan_fill(p, s, n_all_free, blockIdx.x * FILL_THREADS + tid, gridDim.x * FILL_THREADS, t0 + 4 * tid, t0 + min(left, FILL_TOKENS));
 }
 
 void launch_paged_plan(const PagedPlan& p, hipStream_t st) {

@@ -57,14 +57,14 @@ struct PfItem {
 #define LOCRET_PF_WAIT(a, b, n) asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "i"(n))
 
 // Finds item x = (token tile, KV head): the token tiles of all requests in their order, a request's last tile first (it sees the most keys).
-// scratch: LDS, PF_NW 64-bit words and n_req + 1 ints, free again after the next barrier.  False: there is no such tile.  All results are the
+// scratch: LDS, PF_NW words and n_req + 1 ints, free again after the next barrier.  False: there is no such tile.  All results are the
 // same in the whole workgroup.
-constexpr int PF_SCRATCH = PF_NW * 8;
+constexpr int PF_SCRATCH = PF_NW * 4;
 __device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm, int x, unsigned char* scratch, PfItem& it) {
-  int64_t* scan = (int64_t*)scratch;
+  uint32_t* scan = (uint32_t*)scratch;
   int32_t* first = (int32_t*)(scratch + PF_SCRATCH);
   const int tid = threadIdx.x, tw = PF_ROWS / Dm.g, ipt = (a.n_req + PF_THREADS - 1) / PF_THREADS;
-  int64_t mine = 0, total;
+  uint32_t mine = 0, total;
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < a.n_req) {
@@ -73,7 +73,7 @@ __device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm,
       mine += first[r + 1];
     }
   }
-  int64_t before = block_exclusive(mine, scan, total);
+  uint32_t before = block_exclusive(mine, scan, total);
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < a.n_req) {
@@ -92,12 +92,8 @@ __device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm,
     it.m = x % Dm.h_kv;
   }
   tile = x / Dm.h_kv;
-  if (tile >= total) return false;
-  int lo = 0, hi = a.n_req - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= tile) lo = mid; else hi = mid - 1;
-  }
+  if (tile >= (int)total) return false;
+  const int lo = last_at_or_before(first, a.n_req, tile);
   const int tt = first[lo + 1] - 1 - tile;
   const int c0 = paged_cu(a.cu, lo, a.T), n = paged_cu(a.cu, lo + 1, a.T) - c0;
   it.r = __builtin_amdgcn_readfirstlane(lo);

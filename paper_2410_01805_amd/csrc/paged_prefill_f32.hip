@@ -19,13 +19,13 @@ constexpr float PR_RESCALE_LOG2 = 8.f;
 struct PrItem {
   int r, m, row0, n_rows, t0, pos0;      // request, KV head, first row and rows of it, first token (packed) and its position
 };
-// Item x: (16 rows, KV head).  first: LDS, n_req + 1 ints behind PR_NW 64-bit words.
-constexpr int PR_SCRATCH = PR_NW * 8;
+// Item x: (16 rows, KV head).  first: LDS, n_req + 1 ints behind PR_NW words.
+constexpr int PR_SCRATCH = PR_NW * 4;
 __device__ __forceinline__ bool pr_item(const PagedAttn& a, const PagedDims& Dm, int x, unsigned char* scratch, PrItem& it) {
-  int64_t* scan = (int64_t*)scratch;
+  uint32_t* scan = (uint32_t*)scratch;
   int32_t* first = (int32_t*)(scratch + PR_SCRATCH);
   const int tid = threadIdx.x, ipt = (a.n_req + PR_THREADS - 1) / PR_THREADS;
-  int64_t mine = 0, total;
+  uint32_t mine = 0, total;
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < a.n_req) {
@@ -34,7 +34,7 @@ __device__ __forceinline__ bool pr_item(const PagedAttn& a, const PagedDims& Dm,
       mine += first[r + 1];
     }
   }
-  int64_t before = block_exclusive(mine, scan, total);
+  uint32_t before = block_exclusive(mine, scan, total);
   for (int u = 0; u < ipt; ++u) {
     const int r = tid * ipt + u;
     if (r < a.n_req) {
@@ -45,12 +45,8 @@ __device__ __forceinline__ bool pr_item(const PagedAttn& a, const PagedDims& Dm,
   if (tid == 0) first[0] = 0;
   __syncthreads();
   const int tile = x / Dm.h_kv;
-  if (tile >= total) return false;
-  int lo = 0, hi = a.n_req - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= tile) lo = mid; else hi = mid - 1;
-  }
+  if (tile >= (int)total) return false;
+  const int lo = last_at_or_before(first, a.n_req, tile);
   const int c0 = paged_cu(a.cu, lo, a.T), n = paged_cu(a.cu, lo + 1, a.T) - c0;
   it.r = __builtin_amdgcn_readfirstlane(lo);
   it.m = __builtin_amdgcn_readfirstlane(x % Dm.h_kv);
@@ -81,7 +77,7 @@ __device__ __forceinline__ int pr_part_len(int total, int parts) { return (total
 template <int D>
 __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm,
                                                                                      int n_items, int parts, float* __restrict__ part) {
-  typedef PagedTileF32<D> Tile;
+  typedef PagedTileF32<D, true> Tile;
   constexpr int NV = D / 16;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* sets = (float*)smem;                              // [wavefront][16][D]

@@ -5,13 +5,18 @@
 namespace locret {
 
 // DecTile's operands from two places: rows 0..15 and 16..31 of the tile (pages of 16 units; the same place for larger ones).
-template <int D> struct PagedTileBf16 : DecTile<D> {
+// SMALL: the two places differ.  Otherwise `lo` is the same in the whole wavefront and the lanes add 32-bit offsets to it.
+template <bool SMALL> __device__ __forceinline__ const void* tile_row(const void* lo, const void* hi, bool second, uint32_t bytes) {
+  if constexpr (SMALL) return (const char*)(second ? hi : lo) + bytes;
+  else return (const char*)lo + bytes;
+}
+template <int D, bool SMALL> struct PagedTileBf16 : DecTile<D> {
   typedef DecTile<D> Base;
   static constexpr int NQ = Base::NKS;
   typedef bf16x8 q_t;
   __device__ __forceinline__ void load_k(const bf16_t* lo, const bf16_t* hi) {
     const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const bf16_t* base = (n >= 8 ? hi : lo) + (8 * (n >> 2) + (n & 3)) * D + kg * 8;
+    const bf16_t* base = (const bf16_t*)tile_row<SMALL>(lo, hi, n >= 8, ((8 * (n >> 2) + (n & 3)) * D + kg * 8) * 2);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -19,7 +24,7 @@ template <int D> struct PagedTileBf16 : DecTile<D> {
   }
   __device__ __forceinline__ void load_v(const bf16_t* lo, const bf16_t* hi) {
     const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const bf16_t* base = (kg >= 2 ? hi : lo) + 8 * kg * D + n * Base::NV;
+    const bf16_t* base = (const bf16_t*)tile_row<SMALL>(lo, hi, kg >= 2, (8 * kg * D + n * Base::NV) * 2);
 #pragma unroll
     for (int r = 0; r < 8; ++r) load_words<Base::NV / 2>(base + r * D, this->vw[r]);
   }
@@ -42,14 +47,14 @@ template <int D> struct PagedTileBf16 : DecTile<D> {
 
 // The same for float: v_mfma_f32_16x16x4_f32.  Contraction step (ks, e) of S^T has dim 16 ks + 4 kg + e in lane group kg, so that a lane
 // reads 16 bytes; step r of a block's O = P V has key 4 kg + r there, which is where that key's probability is.
-template <int D> struct PagedTileF32 {
+template <int D, bool SMALL> struct PagedTileF32 {
   static constexpr int NQ = D / 16, NV = D / 16;
   typedef float4 q_t;
   float4 ka[2][NQ];
   float vw[8][NV];
   __device__ __forceinline__ void load_k(const float* lo, const float* hi) {
     const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const float* base = (n >= 8 ? hi : lo) + (8 * (n >> 2) + (n & 3)) * D + kg * 4;
+    const float* base = (const float*)tile_row<SMALL>(lo, hi, n >= 8, ((8 * (n >> 2) + (n & 3)) * D + kg * 4) * 4);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -57,7 +62,7 @@ template <int D> struct PagedTileF32 {
   }
   __device__ __forceinline__ void load_v(const float* lo, const float* hi) {
     const int n = threadIdx.x & 15, kg = (threadIdx.x & 63) >> 4;
-    const float* base = (kg >= 2 ? hi : lo) + 8 * kg * D + n * NV;
+    const float* base = (const float*)tile_row<SMALL>(lo, hi, kg >= 2, (8 * kg * D + n * NV) * 4);
 #pragma unroll
     for (int r = 0; r < 8; ++r)
 #pragma unroll
@@ -94,7 +99,7 @@ template <int D> struct PagedTileF32 {
       for (int i = 0; i < NV; ++i) o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(p[r], vw[r][i], o[i], 0, 0, 0);
   }
 };
-template <typename T, int D> struct PagedTileOf { typedef PagedTileBf16<D> type; };
-template <int D> struct PagedTileOf<float, D> { typedef PagedTileF32<D> type; };
+template <typename T, int D, bool SMALL> struct PagedTileOf { typedef PagedTileBf16<D, SMALL> type; };
+template <int D, bool SMALL> struct PagedTileOf<float, D, SMALL> { typedef PagedTileF32<D, SMALL> type; };
 
 }  // namespace locret
