@@ -331,18 +331,37 @@ __global__ __launch_bounds__(PD_THREADS) void paged_decode_join_kernel(PagedAttn
   float M = -INFINITY, L = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   if (g < NP) {
-    for (int w = w0 + g; w <= w1; w += NP) {
-      const int64_t slot = 2 * (int64_t)w + (w == w0 && second ? 1 : 0);
-      const float2 ml = pc.ml[slot * PD_HEADS + head];
-      const float4 y = *(const float4*)&pc.o[(slot * rows_max + head) * D + e * 4];
-      if (ml.y == 0.f) continue;                           // saw nothing (a sum of NaN is not 0)
-      const float Mn = fmaxf(M, ml.x), ref = Mn == -INFINITY ? 0.f : Mn;
-      const float wa = M == -INFINITY ? (L == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(M - ref), wb = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
-      L = (wa == 0.f ? 0.f : wa * L) + wb * ml.y;
-      x.x = (wa == 0.f ? 0.f : wa * x.x) + wb * y.x;
-      x.y = (wa == 0.f ? 0.f : wa * x.y) + wb * y.y;
-      x.z = (wa == 0.f ? 0.f : wa * x.z) + wb * y.z;
-      x.w = (wa == 0.f ? 0.f : wa * x.w) + wb * y.w;
+    constexpr int B = 8;                                   // pieces requested together: each is a trip to memory
+    for (int wb = w0 + g; wb <= w1; wb += NP * B) {
+      float2 ml[B];
+      float4 y[B];
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        const int w = min(wb + i * NP, w1);
+        const int64_t slot = 2 * (int64_t)w + (w == w0 && second ? 1 : 0);
+        ml[i] = pc.ml[slot * PD_HEADS + head];
+        y[i] = *(const float4*)&pc.o[(slot * rows_max + head) * D + e * 4];
+      }
+      float Mn = M;
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        if (wb + i * NP > w1) ml[i].y = 0.f;
+        if (ml[i].y != 0.f) Mn = fmaxf(Mn, ml[i].x);       // (a piece whose sum is 0 saw nothing; one of NaN is not 0)
+      }
+      const float ref = Mn == -INFINITY ? 0.f : Mn;
+      const float wa = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - ref);      // (nothing so far is 0, or not finite)
+      L *= wa;
+      x.x *= wa; x.y *= wa; x.z *= wa; x.w *= wa;
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        if (ml[i].y == 0.f) continue;
+        const float wt = ml[i].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - ref);
+        L = fmaf(wt, ml[i].y, L);
+        x.x = fmaf(wt, y[i].x, x.x);
+        x.y = fmaf(wt, y[i].y, x.y);
+        x.z = fmaf(wt, y[i].z, x.z);
+        x.w = fmaf(wt, y[i].w, x.w);
+      }
       M = Mn;
     }
     so[g][e] = x;
