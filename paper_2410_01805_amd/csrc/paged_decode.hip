@@ -3,7 +3,7 @@
 // Every key and value is read once for all query heads of its group, so HBM is the bound; both products run on the matrix cores with
 // the heads of a group (16 at a time) as one side of a 16 x 16 tile, so that the arithmetic stays far below that bound for any group.
 //
-// Work: an item is (request, KV head, 16 query heads), a unit 128 keys of an item (32 a wavefront).  Lengths are known on the device only, and
+// Work: an item is (request, KV head, 16 query heads), a unit four tiles of 32 keys of an item (one a wavefront).  Lengths are known on the device only, and
 // differ, so the units of all items are laid end to end and every workgroup takes the same number of them, as many workgroups
 // as the chip holds at once.  Each workgroup forms the sums of units over the requests by itself (at most 4096 numbers from L2, one scan) and
 // finds its first unit by bisection.  An item that one workgroup holds whole is written by it; of one that is cut, every
@@ -21,16 +21,16 @@
 
 namespace locret {
 
-constexpr int PD_THREADS = 256, PD_NW = 4, PD_UNIT = 128, PD_HEADS = 16;
+constexpr int PD_THREADS = 256, PD_NW = 4, PD_HEADS = 16;
 constexpr float PD_RESCALE_LOG2 = 8.f;
 
 // Workgroups a CU: what registers allow without spilling.
 template <typename T, int D> struct PagedOcc { static constexpr int value = sizeof(T) == 2 ? (D >= 96 ? 3 : 4) : (D >= 96 ? 2 : 3); };
 static int paged_decode_workgroups(const PagedDims& D) { return 256 * (D.bf16 ? (D.d >= 96 ? 3 : 4) : (D.d >= 96 ? 2 : 3)); }
 
-// The visible units of a request: its sinks, then from the first 32 keys with one in the window on.
+// The visible keys of a request in tiles of 32: sinks, then from the first tile with a key in the window on; four tiles are a unit.
 struct PagedSpan {
-  int n, w0, ns, wb, us, total;      // units in the cache, first key of the window, sinks in front of it, its first tile, units of either
+  int n, w0, ns, wb, st, total;      // units in the cache, first key of the window, sinks in front of it, its first tile, tiles of sinks; units
 };
 __device__ __forceinline__ PagedSpan paged_span(int n, int window, int n_sink) {
   PagedSpan s;
@@ -38,8 +38,8 @@ __device__ __forceinline__ PagedSpan paged_span(int n, int window, int n_sink) {
   s.w0 = window ? max(0, n - window) : 0;
   s.ns = min(n_sink, s.w0);
   s.wb = s.w0 & ~31;
-  s.us = (s.ns + PD_UNIT - 1) / PD_UNIT;
-  s.total = s.us + (n - s.wb + PD_UNIT - 1) / PD_UNIT;
+  s.st = (int)(((uint32_t)s.ns + 31) / 32);
+  s.total = (s.st + (int)(((uint32_t)(n - s.wb) + 31) / 32) + PD_NW - 1) / PD_NW;
   return s;
 }
 
@@ -151,8 +151,9 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
     struct Place { int kb, lo, hi, id0, id1; };
     auto place = [&](int t) __attribute__((always_inline)) {
       Place p;
-      const bool sink = t < sp.us;
-      p.kb = (sink ? t * PD_UNIT : sp.wb + (t - sp.us) * PD_UNIT) + wave * 32;
+      const int i = t * PD_NW + wave;
+      const bool sink = i < sp.st;
+      p.kb = sink ? i * 32 : sp.wb + (i - sp.st) * 32;
       p.lo = sink ? 0 : sp.w0;
       p.hi = sink ? sp.ns : sp.n;
       p.id0 = p.id1 = -1;

@@ -160,23 +160,6 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
 
   auto tile_key = [&](int t) __attribute__((always_inline)) { return t < ks_.ns_t ? t * KT : ks_.wb + (t - ks_.ns_t) * KT; };
   auto tile_end = [&](int t) __attribute__((always_inline)) { return t >= t_hi ? 0 : t < ks_.ns_t ? ks_.ns : ks_.n_keys; };
-  // does a page of the item's keys lie outside the pool?  All rows are then formed key by key.
-  bool redo;                                   // the wavefront's rows have to be formed key by key
-  {
-    int odd = 0;
-    const int s_end = (ks_.ns + page - 1) >> shift, e0 = ks_.wb >> shift, e1 = (ks_.n_keys + page - 1) >> shift;
-    for (int i = tid; i < s_end; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
-    for (int i = e0 + tid; i < e1; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
-    int32_t* said = (int32_t*)ring;
-    __syncthreads();                                       // `ring` no longer holds the sums of pf_item
-    if (tid == 0) *said = 0;
-    __syncthreads();
-    if (odd) *said = 1;
-    __syncthreads();
-    redo = __builtin_amdgcn_readfirstlane(*said) != 0;
-    __syncthreads();
-  }
-
   // this lane's row, and the first and last position of the wavefront's
   const int row = min(wave * 32 + n32, rows - 1), tok = row / g;
   const int64_t at = (int64_t)(it.t0 + tok) * Dm.h + it.m * g + (row - tok * g);
@@ -191,9 +174,6 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     const bf16_t* qp = q + at * D + hi * 8;
 #pragma unroll
     for (int s = 0; s < NKS; ++s) qf[s] = *(const bf16x8*)(qp + s * 16);
-    // waited for here: a wait in the loop, where they are used first, would be one for the tiles in flight too
-#pragma unroll
-    for (int s = 0; s < NKS; ++s) asm volatile("" : "+v"(qf[s]));
   }
   f32x16 oacc[NDB];
 #pragma unroll
@@ -269,6 +249,30 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
       }
     }
   };
+
+  // The first page numbers and the queries are on their way; the pages are looked through meanwhile.
+  if (wave >= PF_NW / 2) request(0);
+  // does a page of the item's keys lie outside the pool?  All rows are then formed key by key.
+  bool redo;                                   // the wavefront's rows have to be formed key by key
+  {
+    int odd = 0;
+    const int s_end = (ks_.ns + page - 1) >> shift, e0 = ks_.wb >> shift, e1 = (ks_.n_keys + page - 1) >> shift;
+    for (int i = tid; i < s_end; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
+    for (int i = e0 + tid; i < e1; i += PF_THREADS) odd |= (unsigned)trow[i] >= (unsigned)Dm.n_pages;
+    // (said in the last stage, which is loaded behind further barriers; after this one `ring` no longer holds the sums of pf_item either)
+    int32_t* said = (int32_t*)(ring + sizeof(ring)) - PF_NW;
+    odd = __any(odd);
+    if (lane == 0) said[wave] = odd;
+    __syncthreads();
+    odd = 0;
+#pragma unroll
+    for (int w = 0; w < PF_NW; ++w) odd |= said[w];
+    redo = __builtin_amdgcn_readfirstlane(odd) != 0;
+  }
+
+  // waited for here: a wait in the loop, where they are used first, would be one for the tiles in flight too
+#pragma unroll
+  for (int s = 0; s < NKS; ++s) asm volatile("" : "+v"(qf[s]));
 
   // ---- fragment addresses (bytes inside a stage) -----------------------------------------------------------------------
   const int k_row = KH == 1 ? n32 : n32 >> 1, k_half = KH == 1 ? 0 : n32 & 1;
@@ -430,7 +434,6 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     return kb <= any_hi && (t < ks_.ns_t || kb >= any_lo || kb < Dm.n_sink);
   };
   if (wave >= PF_NW / 2) {
-    request(0);
     issue(0);
     issue(1);
     issue(2);

@@ -1,7 +1,7 @@
 // Causal attention of a ragged batch of chunks over pages (locret_paged_prefill), float.
 //   s_tj = scale q_t . k_j over the visible keys j of query t,  out_t = sum_j e^(s_tj - M_t) v_j / L_t,  lse_t = M_t + ln L_t
 // Both products with v_mfma_f32_16x16x4_f32 (157 TFLOP/s on the card), which bounds long chunks; short ones are bound by the chain of their
-// launch.  A workgroup has 16 rows (token, query head of one KV head) and goes over the keys that any of them sees, 128 at a time, a quarter
+// launch.  A workgroup has 16 rows (token, query head of one KV head) and goes over the keys that any of them sees, 128 at a time, 32
 // for each of its four wavefronts; their maxima, sums and accumulators are joined in LDS.  So few rows make many workgroups, and a chunk of 400
 // tokens fills the chip.  Where there are fewer workgroups than CUs the keys of each are cut into parts, which a second launch joins.
 // Keys and values go from the pages to registers in the layout of the operands (PagedTileF32); neighbouring workgroups read the same ones, from L2.
@@ -12,7 +12,7 @@
 
 namespace locret {
 
-constexpr int PR_THREADS = 256, PR_NW = 4, PR_ROWS = 16, PR_UNIT = 128;
+constexpr int PR_THREADS = 256, PR_NW = 4, PR_ROWS = 16;
 constexpr int PR_CUS = 256, PR_MAX_PARTS = 16, PR_MAX_SLOTS = 512;
 constexpr float PR_RESCALE_LOG2 = 8.f;
 
@@ -57,9 +57,9 @@ __device__ __forceinline__ bool pr_item(const PagedAttn& a, const PagedDims& Dm,
   return true;
 }
 
-// The keys of an item in units of 128: sinks, then from the first 32 keys with one in a row's window on.
+// The keys of an item in tiles of 32: sinks, then from the first tile with a key in a row's window on; four tiles are a unit.
 struct PrSpan {
-  int w0, ns, wb, end, us, total;
+  int w0, ns, wb, end, st, total;
 };
 __device__ __forceinline__ PrSpan pr_span(const PrItem& it, const PagedDims& Dm) {
   PrSpan s;
@@ -68,8 +68,8 @@ __device__ __forceinline__ PrSpan pr_span(const PrItem& it, const PagedDims& Dm)
   s.w0 = Dm.window ? max(0, p0 - Dm.window + 1) : 0;
   s.ns = min(Dm.n_sink, s.w0);
   s.wb = s.w0 & ~31;
-  s.us = (s.ns + PR_UNIT - 1) / PR_UNIT;
-  s.total = s.us + (max(s.end - s.wb, 0) + PR_UNIT - 1) / PR_UNIT;
+  s.st = (int)(((uint32_t)s.ns + 31) / 32);
+  s.total = (s.st + (int)(((uint32_t)max(s.end - s.wb, 0) + 31) / 32) + PR_NW - 1) / PR_NW;
   return s;
 }
 __device__ __forceinline__ int pr_part_len(int total, int parts) { return (total + parts - 1) / parts; }
@@ -111,12 +111,13 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
     if (sink) return key < sp.ns && key <= pos;
     return key >= sp.w0 && key <= pos && (Dm.window == 0 || pos - key < Dm.window || key < Dm.n_sink);
   };
-  struct Place { int kb, end, id0, id1; };
+  struct Place { bool sink; int kb, end, id0, id1; };
   auto place = [&](int u) __attribute__((always_inline)) {
     Place p;
-    const bool sink = u < sp.us;
-    p.kb = (sink ? u * PR_UNIT : sp.wb + (u - sp.us) * PR_UNIT) + wave * 32;
-    p.end = sink ? sp.ns : sp.end;
+    const int i = u * PR_NW + wave;
+    p.sink = i < sp.st;
+    p.kb = p.sink ? i * 32 : sp.wb + (i - sp.st) * 32;
+    p.end = p.sink ? sp.ns : sp.end;
     p.id0 = p.id1 = -1;
     if (p.kb < p.end) {
       p.id0 = trow[p.kb >> shift];
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
 #pragma unroll
   for (int i = 0; i < NV; ++i) o[i] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
   float mrun = -INFINITY, lrun = 0.f;
-  Place p = {0, 0, -1, -1}, nx = p;
+  Place p = {false, 0, 0, -1, -1}, nx = p;
   if (u0 < u1) {
     p = place(u0);
     if (p.kb < p.end) {
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
   }
   for (int u = u0; u < u1; ++u) {
     const Place nn = place(min(u + 2, u1 - 1));
-    const bool sink = u < sp.us, work = p.kb < p.end, more = u + 1 < u1 && nx.kb < nx.end;
+    const bool sink = p.sink, work = p.kb < p.end, more = u + 1 < u1 && nx.kb < nx.end;
     dec_f32x4 s[2];
     float pr[8];
     if (work) tl.logits(qb, s);
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
 #pragma unroll
         for (int e = 0; e < D / 4; ++e) s = fmaf(qv[e], Kp[off + e], s);
         s = sum_across_quarters(s);
-        const bool see = sees(u < sp.us, key);
+        const bool see = sees(w.sink, key);
         const float x = see ? s * c : -INFINITY, m_new = fmaxf(mrun, x), ref = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(mrun - ref), pk = __builtin_amdgcn_exp2f(x - ref);
         l = l * alpha + pk;
