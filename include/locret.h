@@ -273,7 +273,7 @@ typedef struct {
   int32_t page_size;      /* units of a page: 16, 32, 64, 128 or 256                             */
   int32_t n_pages;        /* pages of the pool; n_pages * page_size < 2^31                       */
   int32_t max_reqs;       /* largest n_req of any call, at most LOCRET_PAGED_MAX_REQS            */
-  int32_t max_pages;      /* row length of block_table; max_pages * page_size < 2^31, max_reqs times that at most 2^37 */
+  int32_t max_pages;      /* row length of block_table; max_pages * page_size at most 2^30, max_reqs times that at most 2^37 */
   int32_t window;         /* 0: a query sees every unit up to its own.  Else the last `window` of those only, its own counted */
   int32_t n_sink;         /* with a window: units that stay visible at the start of every request */
   float   softmax_scale;  /* 0 selects 1/sqrt(head_dim)                                          */

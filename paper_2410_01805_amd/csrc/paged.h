@@ -72,6 +72,10 @@ size_t paged_prefill_workspace(const PagedDims& D);
 void launch_paged_prefill_f32(const PagedDims& D, const PagedAttn& a, hipStream_t st);
 size_t paged_prefill_f32_workspace(const PagedDims& D);
 
+// Workgroups of a launch over two grid dimensions: one dimension holds fewer than 2^32 threads.
+inline dim3 paged_grid(int64_t n) { return n <= 1 << 20 ? dim3((unsigned)n) : dim3(1u << 20, (unsigned)((n + (1 << 20) - 1) >> 20)); }
+__device__ __forceinline__ int paged_block() { return (int)(blockIdx.y * gridDim.x + blockIdx.x); }
+
 // Data that a launch only reads, from places that are the same in a wavefront: through the scalar cache.
 typedef const __attribute__((address_space(4))) int32_t* paged_const_i32;
 

@@ -24,7 +24,7 @@ int validate(const locret_paged_config* c, PagedDims* D) {
   int shift = 0;
   for (int s = 4; s <= 8; ++s) if (c->page_size == 1 << s) shift = s;
   if (!shift || c->max_reqs > PAGED_MAX_REQS) return LOCRET_ESHAPE;
-  if (((int64_t)c->n_pages << shift) > INT32_MAX || ((int64_t)c->max_pages << shift) > INT32_MAX) return LOCRET_ESHAPE;
+  if (((int64_t)c->n_pages << shift) > INT32_MAX || ((int64_t)c->max_pages << shift) > 1 << 30) return LOCRET_ESHAPE;
   if (((int64_t)c->max_reqs * c->max_pages << shift) > (int64_t)1 << 37) return LOCRET_ESHAPE;     // units of work are counted in 32 bits
   D->h = c->n_q_heads;
   D->h_kv = c->n_kv_heads;
@@ -52,7 +52,7 @@ int attention(const locret_paged_config* cfg, const PagedAttn& a, size_t bytes, 
   const int rc = validate(cfg, &D);
   if (rc != LOCRET_OK) return rc;
   if (a.n_req < 0 || a.T < 0) return LOCRET_EINVAL;
-  if (a.n_req > cfg->max_reqs || (int64_t)a.T * D.h > (int64_t)1 << 37) return LOCRET_ESHAPE;      // (launches are counted in 32 bits)
+  if (a.n_req > cfg->max_reqs || (int64_t)a.T * D.h > (int64_t)1 << 34) return LOCRET_ESHAPE;      // (launches are counted in 32 bits)
   if (a.n_req == 0 || a.T == 0) return LOCRET_OK;
   if (!a.q || !a.K || !a.V || !a.table || !a.lens || (prefill && !a.cu) || !a.out || !a.ws) return LOCRET_EINVAL;
   if (misaligned(a.q) || misaligned(a.K) || misaligned(a.V) || misaligned(a.out) || misaligned(a.ws, 256) || misaligned(a.table, 4) ||

@@ -5,7 +5,8 @@
 //
 // Bound by HBM: every element is read once and written once, the sums of a row stay in the lanes that hold it.  A lane holds two
 // 16-byte chunks of a row, the partners of a rotation where the pairs are (i, i + rot/2), neighbours otherwise, so that
-// neither the rotation nor an update in place needs another lane's data.  Angles are formed once a token and pair, in LDS, for all
+// neither the rotation nor an update in place needs another lane's data.  A workgroup has one token (8192 tokens of 32 query and 8 KV heads of
+// 128 dims: 40.2 us, 5.0 TB/s, what a large copy reaches; with 2, 4, 8 tokens 41.9, 43.7, 44.7), whose angles it forms once, in LDS, for all
 // heads: the turns position * f / 2 pi in 64 bits, of which only the fraction goes on in 32 (a product in 32 bits would be off by
 // half a radian at position 2^20 with 2^-24 of rounding).
 #include "device_util.h"
@@ -16,21 +17,21 @@ namespace locret {
 constexpr int APPEND_THREADS = 256;
 
 template <typename T, int D, bool IL>
-__global__ __launch_bounds__(APPEND_THREADS) void paged_append_kernel(PagedRows a, int h, int h_kv, int page_shift, int n_pages, int tokens) {
+__global__ __launch_bounds__(APPEND_THREADS) void paged_append_kernel(PagedRows a, int h, int h_kv, int page_shift, int n_pages) {
   constexpr int VEC = Vec16<T>::N;
   constexpr int LPR = D / (2 * VEC);                         // lanes that hold a row
   constexpr int LPRP = LPR <= 2 ? 2 : LPR <= 4 ? 4 : LPR <= 8 ? 8 : 16;
   constexpr int RPP = APPEND_THREADS / LPRP;                 // rows the workgroup takes at a time
   typedef Vec16<T> V16;
   typedef decltype(V16().raw) raw_t;
-  extern __shared__ float2 turn[];                           // [tokens][rot / 2]: amplitude * (cos, sin)
-  const int tid = threadIdx.x, half = a.rot >> 1;
-  const int t0 = blockIdx.x * tokens, nt = min(tokens, a.T - t0);
-  for (int i = tid; i < nt * half; i += APPEND_THREADS) {
-    const double turns = (double)a.positions[t0 + i / half] * a.freq[i % half] * 0.15915494309189533577;
+  __shared__ float2 turn[D / 2];                             // [rot / 2]: amplitude * (cos, sin)
+  const int tid = threadIdx.x, half = a.rot >> 1, t = paged_block();
+  if (t >= a.T) return;
+  if (tid < half) {
+    const double turns = (double)a.positions[t] * a.freq[tid] * 0.15915494309189533577;
     float s, c;
     sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-    turn[i] = make_float2(a.amplitude * c, a.amplitude * s);
+    turn[tid] = make_float2(a.amplitude * c, a.amplitude * s);
   }
   __syncthreads();
   const int sub = tid % LPRP, HR = half / VEC;
@@ -39,8 +40,9 @@ __global__ __launch_bounds__(APPEND_THREADS) void paged_append_kernel(PagedRows 
   // the lane's two chunks
   const int c0 = !IL && lane_c < HR ? lane_c : 2 * lane_c, c1 = !IL && lane_c < HR ? lane_c + HR : 2 * lane_c + 1;
   const int nq = a.q ? h : 0, nk = a.k ? h_kv : 0, R = nq + 2 * nk;
-  for (int row = tid / LPRP; row < nt * R; row += RPP) {
-    const int tl = row / R, rr = row % R, t = t0 + tl;
+  const int slot = a.k ? a.slots[t] : -1;
+  const bool has = slot >= 0 && (slot >> page_shift) < n_pages;
+  for (int rr = tid / LPRP; rr < R; rr += RPP) {
     const bool isq = rr < nq, isk = !isq && rr < nq + nk;
     const int head = isq ? rr : isk ? rr - nq : rr - nq - nk;
     const T* src = isq ? (const T*)a.q + t * a.q_tok + head * a.q_head
@@ -49,8 +51,6 @@ __global__ __launch_bounds__(APPEND_THREADS) void paged_append_kernel(PagedRows 
     if (isq) {
       dst = (T*)a.q_out + ((int64_t)t * h + head) * D;
     } else {
-      const int slot = a.slots[t];
-      const bool has = slot >= 0 && (slot >> page_shift) < n_pages;
       const int64_t at = (((int64_t)(slot >> page_shift) * h_kv + head) << page_shift) + (slot & ((1 << page_shift) - 1));
       dst = has ? (T*)(isk ? a.K : a.V) + at * D : nullptr;
     }
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void paged_append_kernel(PagedRows 
           w[e] = w[e] * inv * weight[c1 * VEC + e];
         }
       }
-      const float2* cs = turn + tl * half;
+      const float2* cs = turn;
       if constexpr (IL) {
         if (c0 * VEC < a.rot) {
 #pragma unroll
@@ -110,11 +110,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void paged_append_kernel(PagedRows 
 
 template <typename T, int D>
 static void append_d(const PagedDims& Dm, const PagedRows& a, hipStream_t st) {
-  const int tokens = a.T >= 2048 ? 4 : 1;
-  const unsigned n = (unsigned)(((int64_t)a.T + tokens - 1) / tokens);
-  const size_t lds = (size_t)tokens * (a.rot / 2) * sizeof(float2);
-  if (a.interleaved) paged_append_kernel<T, D, true><<<n, APPEND_THREADS, lds, st>>>(a, Dm.h, Dm.h_kv, Dm.page_shift, Dm.n_pages, tokens);
-  else paged_append_kernel<T, D, false><<<n, APPEND_THREADS, lds, st>>>(a, Dm.h, Dm.h_kv, Dm.page_shift, Dm.n_pages, tokens);
+  if (a.interleaved) paged_append_kernel<T, D, true><<<paged_grid(a.T), APPEND_THREADS, 0, st>>>(a, Dm.h, Dm.h_kv, Dm.page_shift, Dm.n_pages);
+  else paged_append_kernel<T, D, false><<<paged_grid(a.T), APPEND_THREADS, 0, st>>>(a, Dm.h, Dm.h_kv, Dm.page_shift, Dm.n_pages);
 }
 
 void launch_paged_append(const PagedDims& D, const PagedRows& a, hipStream_t st) {

@@ -27,7 +27,7 @@
 // Tiles that some row of a wavefront does not see whole are masked before the maximum.  A masked probability is 0, but 0 times a value that is
 // not finite is not: where an accumulator is not finite in the end, the wavefront forms its rows once more behind the loop, key by key, from
 // the keys that each row sees.  (There no tile's registers are alive; the same inside the loop took half of its speed in spills, and looking
-// through the values of masked tiles a third of the time of 12 ragged requests with a window, 94 -> @@ us.)
+// through the values of masked tiles a third of the time of 12 ragged requests with a window, 94 -> 59 us.)
 //
 // Few rows: where the items (tokens tile, KV head) are at most half as many as the CUs, each one's keys are cut into parts,
 // workgroups of their own, which leave maximum, sum and accumulators; a second launch joins them.
@@ -44,7 +44,7 @@ typedef short pf_s16x8 __attribute__((ext_vector_type(8)));
 constexpr int PF_NW = 8, PF_THREADS = PF_NW * 64, PF_ROWS = PF_NW * 32;
 constexpr int PF_TILE_B = 64 * 256, PF_STAGE_B = 2 * PF_TILE_B;
 constexpr int PF_KPRE = 4;                     // K fragments fetched ahead of the S block
-constexpr int PF_CUS = 256, PF_MAX_PARTS = 16, PF_MAX_SLOTS = 256;
+constexpr int PF_CUS = 256, PF_MAX_PARTS = 16, PF_MAX_SLOTS = PF_CUS;
 constexpr int PF_MIN_PART = 4;                 // key tiles of a part at least: less does not pay for a part's prologue and joining
 
 // What a workgroup works on.
@@ -136,12 +136,13 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   constexpr int KC_B = 4096 / KH, KC_H = 2048 / KH;        // bytes of 16 keys and of 8 keys in LDS
   constexpr int YTAIL = D == 128 ? 4 : 1;                  // MFMAs of A's S block behind barrier Y
   // The only LDS variable: with a second one the compiler tells them apart by alias scopes, and then waits for all direct loads before every
-  // read of `ring`, which it cannot tell from the stages in flight (4096 tokens on 16384 units: 909 us instead of @@).
+  // read of `ring`, which it cannot tell from the stages in flight (4096 tokens on 16384 units: 948 us, 883 without
+  // that and the queries' wait below).
   __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * PF_STAGE_B];
 
   PfItem it;
-  const int layer = blockIdx.x / n_items;
-  if (!pf_item(a, Dm, blockIdx.x - layer * n_items, ring, it)) return;
+  const int block = paged_block(), layer = block / n_items;
+  if (layer >= parts || !pf_item(a, Dm, block - layer * n_items, ring, it)) return;
   const PfKeys ks_ = pf_keys(it, Dm, KT);
   int t_lo = 0, t_hi = ks_.n_tiles;
   bool cut = false;
@@ -528,7 +529,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   // ---- results ---------------------------------------------------------------------------------------------------------
   const float l = l_run + __shfl_xor(l_run, 32, 64);
   if (cut) {
-    const int64_t slot = blockIdx.x;
+    const int64_t slot = block;
     float4* op = (float4*)part + (slot * PF_NW + wave) * (NDB * 4 * 64) + lane;
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
@@ -615,7 +616,7 @@ static void prefill_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t st) {
   const int n_items = (int)(tiles * Dm.h_kv);
   int parts = PF_CUS / n_items;
   parts = parts < 1 ? 1 : parts > PF_MAX_PARTS ? PF_MAX_PARTS : parts;
-  const unsigned n_wg = (unsigned)n_items * (unsigned)parts;
+  const dim3 n_wg = paged_grid((int64_t)n_items * parts);
   const bf16_t *q = (const bf16_t*)a.q, *K = (const bf16_t*)a.K, *V = (const bf16_t*)a.V;
   if (1 << Dm.page_shift >= pf_tile_keys(D)) paged_prefill_kernel<D, true><<<n_wg, PF_THREADS, 0, st>>>(a, q, K, V, a.table, Dm, n_items, parts, (float*)a.ws);
   else paged_prefill_kernel<D, false><<<n_wg, PF_THREADS, 0, st>>>(a, q, K, V, a.table, Dm, n_items, parts, (float*)a.ws);

@@ -13,7 +13,7 @@
 namespace locret {
 
 constexpr int PR_THREADS = 256, PR_NW = 4, PR_ROWS = 16;
-constexpr int PR_CUS = 256, PR_MAX_PARTS = 16, PR_MAX_SLOTS = 512;
+constexpr int PR_CUS = 256, PR_MAX_PARTS = 16, PR_MAX_SLOTS = PR_CUS;
 constexpr float PR_RESCALE_LOG2 = 8.f;
 
 struct PrItem {
@@ -83,8 +83,8 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
   float* sets = (float*)smem;                              // [wavefront][16][D]
   float2* wml = (float2*)(smem + PR_NW * PR_ROWS * D * sizeof(float));      // [wavefront][16]
   PrItem it;
-  const int layer = blockIdx.x / n_items;
-  if (!pr_item(a, Dm, blockIdx.x - layer * n_items, smem, it)) return;
+  const int block = paged_block(), layer = block / n_items;
+  if (layer >= parts || !pr_item(a, Dm, block - layer * n_items, smem, it)) return;
   __syncthreads();                                         // smem is `sets` from here on
   const PrSpan sp = pr_span(it, Dm);
   int u0 = 0, u1 = sp.total;
@@ -279,8 +279,8 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
       x.w = fmaf(wt, y.w, x.w);
     }
     if (cut) {
-      *(float4*)&part[((int64_t)blockIdx.x * PR_ROWS + rr) * D + e] = x;
-      if (e == 0) ((float2*)(part + (int64_t)PR_MAX_SLOTS * PR_ROWS * D))[(int64_t)blockIdx.x * PR_ROWS + rr] = make_float2(M, L);
+      *(float4*)&part[((int64_t)block * PR_ROWS + rr) * D + e] = x;
+      if (e == 0) ((float2*)(part + (int64_t)PR_MAX_SLOTS * PR_ROWS * D))[(int64_t)block * PR_ROWS + rr] = make_float2(M, L);
       continue;
     }
     const int row_ = it.row0 + rr, tok_ = row_ / Dm.g;
@@ -339,11 +339,11 @@ static void prefill_f32_d(const PagedDims& Dm, const PagedAttn& a, hipStream_t s
   const int64_t most = (int64_t)a.T * ((Dm.g + PR_ROWS - 1) / PR_ROWS);
   if (tiles > most) tiles = most;
   const int n_items = (int)(tiles * Dm.h_kv);
-  // (two workgroups a CU: fewer than that leave matrix cores idle)
-  int parts = 2 * PR_CUS / n_items;
+  // (three ragged requests, 212 workgroups: whole 17.1 us, in two parts and joined 21.3)
+  int parts = PR_CUS / n_items;
   parts = parts < 1 ? 1 : parts > PR_MAX_PARTS ? PR_MAX_PARTS : parts;
   const size_t scratch = PR_SCRATCH + (size_t)(a.n_req + 1) * sizeof(int32_t), body = (size_t)PR_NW * PR_ROWS * (D * sizeof(float) + sizeof(float2));
-  paged_prefill_f32_kernel<D><<<(unsigned)n_items * (unsigned)parts, PR_THREADS, scratch > body ? scratch : body, st>>>(a, a.table, Dm, n_items, parts,
+  paged_prefill_f32_kernel<D><<<paged_grid((int64_t)n_items * parts), PR_THREADS, scratch > body ? scratch : body, st>>>(a, a.table, Dm, n_items, parts,
                                                                                                                    (float*)a.ws);
   if (parts > 1) paged_prefill_f32_join_kernel<D><<<(unsigned)n_items, PR_THREADS, scratch, st>>>(a, Dm, n_items, parts, (const float*)a.ws);
 }

@@ -203,6 +203,15 @@ def test_append_of_queries_alone_keys_alone_and_in_place():
     assert torch.equal(both, q)
 
 
+def test_append_of_more_tokens_than_a_grid_dimension_has_workgroups():
+    T = (1 << 24) + 5
+    cfg = config("bf16", 1, 1, 32, 16, 2)
+    q = torch.randn(T, 1, 32, device=DEV).bfloat16()
+    out = torch.zeros_like(q)
+    B.locret_paged_append(cfg, T, q, None, None, None, None, None, 0, False, 1.0, None, None, 0.0, out, None, None)
+    assert torch.equal(q, out)
+
+
 # ---- attention -------------------------------------------------------------------------------------------------------
 def paged_case(rng, dtype, h, h_kv, d, page, lens, window=0, sink=0, scale=0.0, spread=1.0):
     """Pages in a random order with other numbers everywhere behind the lengths."""

@@ -21,7 +21,7 @@ BAD = [
     (dict(n_q_heads=0), EINVAL), (dict(n_kv_heads=0), EINVAL), (dict(n_kv_heads=3), ESHAPE), (dict(n_q_heads=2048), ESHAPE),
     (dict(n_q_heads=256, n_kv_heads=1), ESHAPE), (dict(head_dim=16), ESHAPE), (dict(head_dim=80), ESHAPE), (dict(head_dim=256), ESHAPE),
     (dict(dtype=2), EINVAL), (dict(page_size=0), ESHAPE), (dict(page_size=8), ESHAPE), (dict(page_size=48), ESHAPE), (dict(page_size=512), ESHAPE),
-    (dict(n_pages=0), EINVAL), (dict(n_pages=1 << 27), ESHAPE), (dict(max_pages=0), EINVAL), (dict(max_pages=1 << 27), ESHAPE), (dict(max_pages=1 << 26, max_reqs=129), ESHAPE),
+    (dict(n_pages=0), EINVAL), (dict(n_pages=1 << 27), ESHAPE), (dict(max_pages=0), EINVAL), (dict(max_pages=1 << 27), ESHAPE), (dict(max_pages=(1 << 26) + 1), ESHAPE), (dict(max_pages=1 << 26, max_reqs=129), ESHAPE),
     (dict(max_reqs=0), EINVAL), (dict(max_reqs=4097), ESHAPE), (dict(window=-1), EINVAL), (dict(n_sink=-1), EINVAL),
     (dict(softmax_scale=-1.0), EINVAL), (dict(softmax_scale=float("nan")), EINVAL), (dict(softmax_scale=float("inf")), EINVAL),
 ]
@@ -94,6 +94,7 @@ def test_attention_refuses(kw, code):
 
 
 def test_prefill_refuses():
+    assert prefill(cfg(n_q_heads=16), T=(1 << 31) - 1, n_req=1) == ESHAPE
     assert prefill(cfg(), T=-1) == EINVAL and prefill(cfg(), cu=None) == EINVAL and prefill(cfg(), cu=P + 2) == EALIGN
 
 
