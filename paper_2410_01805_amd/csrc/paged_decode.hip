@@ -13,8 +13,7 @@
 // Tiles go from memory to registers in the layout of the operands (paged_tile.h; float products are those of 32 bits):
 // S^T = K Q^T has keys as rows, in an order in which a lane's accumulators are the eight keys whose probabilities it gives to
 // O = P V.  The next keys are requested as soon as the logits are formed, the next values after their product, page numbers a unit
-// earlier.  Probabilities of bf16 layers become bf16 factors (half a step of 2^-8 each, as large as the rounding of the output, and
-// independent of each other, so less than that in a sum); maximum, sum and accumulators are 32-bit.  The maximum moves only when a logit
+// earlier.  Probabilities of bf16 layers become two bf16 factors each; maximum, sum and accumulators are 32-bit.  The maximum moves only when a logit
 // exceeds it by 8 binary orders.  What is not seen is taken out by selection: its logit before the maximum, its value before the product.
 #include "paged.h"
 #include "paged_tile.h"
@@ -173,91 +172,105 @@ __global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_dec
     typename Tile::q_t qb[Tile::NQ];
     Tile::load_q((const T*)a.q + ((int64_t)r * Dm.h + j0 + min(n, ng - 1)) * D, n < ng, qb);
     Tile tl;
-    Place p = place(tile);
-    if (p.kb < p.hi) {
-      const T *lo, *hi;
-      address(Kp, p, lo, hi);
-      tl.load_k(lo, hi);
-      address(Vp, p, lo, hi);
-      tl.load_v(lo, hi);
-    }
     dec_f32x4 o[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) o[i] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
-    float mrun = -INFINITY, lrun = 0.f;
-    Place nx = place(min(tile + 1, t_end - 1));
-    for (int t = tile; t < t_end; ++t) {
-      const Place nn = place(min(t + 2, t_end - 1));
-      const bool work = p.kb < p.hi && p.kb + 32 > p.lo, more = t + 1 < t_end && nx.kb < nx.hi;
-      dec_f32x4 s[2];
-      float pr[8];
-      if (p.kb < p.hi) tl.logits(qb, s);
-      const T *klo, *khi;
-      if (more) {
-        address(Kp, nx, klo, khi);
-        tl.load_k(klo, khi);
+    float mrun, lrun;
+    for (bool fine = Tile::HAS_FINE;;) {                   // (a second time where a value is not finite, see PagedTileBf16::add)
+      Place p = place(tile);
+      if (p.kb < p.hi) {
+        const T *lo, *hi;
+        address(Kp, p, lo, hi);
+        tl.load_k(lo, hi);
+        address(Vp, p, lo, hi);
+        tl.load_v(lo, hi);
       }
-      if (work) {
-        uint32_t seen = 0xffu;
-        if (p.kb < p.lo || p.kb + 32 > p.hi || (unsigned)p.id0 >= (unsigned)Dm.n_pages || (unsigned)p.id1 >= (unsigned)Dm.n_pages) {
-          seen = 0;
-          const int id = kg >= 2 ? p.id1 : p.id0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) o[i] = dec_f32x4{0.f, 0.f, 0.f, 0.f};
+      mrun = -INFINITY;
+      lrun = 0.f;
+      Place nx = place(min(tile + 1, t_end - 1));
+      for (int t = tile; t < t_end; ++t) {
+        const Place nn = place(min(t + 2, t_end - 1));
+        const bool work = p.kb < p.hi && p.kb + 32 > p.lo, more = t + 1 < t_end && nx.kb < nx.hi;
+        dec_f32x4 s[2];
+        float pr[8];
+        if (p.kb < p.hi) tl.logits(qb, s);
+        const T *klo, *khi;
+        if (more) {
+          address(Kp, nx, klo, khi);
+          tl.load_k(klo, khi);
+        }
+        if (work) {
+          uint32_t seen = 0xffu;
+          if (p.kb < p.lo || p.kb + 32 > p.hi || (unsigned)p.id0 >= (unsigned)Dm.n_pages || (unsigned)p.id1 >= (unsigned)Dm.n_pages) {
+            seen = 0;
+            const int id = kg >= 2 ? p.id1 : p.id0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int key = p.kb + 8 * kg + j;
+              seen |= (key >= p.lo && key < p.hi && (unsigned)id < (unsigned)Dm.n_pages) ? 1u << j : 0u;
+            }
+            tl.clear_v(seen);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j >> 2][j & 3] = (seen >> j) & 1 ? s[j >> 2][j & 3] : -INFINITY;
+          }
+          float mx = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) mx = fmaxf(mx, s[j >> 2][j & 3]);
+          mx *= c;
+          if (__any((mx - mrun) > PD_RESCALE_LOG2)) {        // also true from -inf to a number
+            mx = max_across_quarters(mx);                    // the four lanes of a column move together
+            const bool up = (mx - mrun) > PD_RESCALE_LOG2;
+            const float alpha = up ? __builtin_amdgcn_exp2f(mrun - mx) : 1.f;
+            if (up) mrun = mx;
+            lrun *= alpha;
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) {
+              const float ar = __shfl(alpha, 4 * kg + rr, 64);      // accumulator row 4 kg + rr is that head
+#pragma unroll
+              for (int i = 0; i < NV; ++i) o[i][rr] *= ar;
+            }
+          }
+          const float ref = mrun == -INFINITY ? 0.f : mrun;  // (nothing seen yet, or every logit so far is -inf)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int key = p.kb + 8 * kg + j;
-            seen |= (key >= p.lo && key < p.hi && (unsigned)id < (unsigned)Dm.n_pages) ? 1u << j : 0u;
+            pr[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], c, -ref));
+            lrun += pr[j];
           }
-          tl.clear_v(seen);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) s[j >> 2][j & 3] = (seen >> j) & 1 ? s[j >> 2][j & 3] : -INFINITY;
+          tl.add(pr, o, fine);
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, s[j >> 2][j & 3]);
-        mx *= c;
-        if (__any((mx - mrun) > PD_RESCALE_LOG2)) {        // also true from -inf to a number
-          mx = max_across_quarters(mx);                    // the four lanes of a column move together
-          const bool up = (mx - mrun) > PD_RESCALE_LOG2;
-          const float alpha = up ? __builtin_amdgcn_exp2f(mrun - mx) : 1.f;
-          if (up) mrun = mx;
-          lrun *= alpha;
-#pragma unroll
-          for (int rr = 0; rr < 4; ++rr) {
-            const float ar = __shfl(alpha, 4 * kg + rr, 64);      // accumulator row 4 kg + rr is that head
-#pragma unroll
-            for (int i = 0; i < NV; ++i) o[i][rr] *= ar;
-          }
+        if (more) {
+          address(Vp, nx, klo, khi);
+          tl.load_v(klo, khi);
         }
-        const float ref = mrun == -INFINITY ? 0.f : mrun;  // (nothing seen yet, or every logit so far is -inf)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          pr[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], c, -ref));
-          lrun += pr[j];
-        }
-        tl.add(pr, o);
+        p = nx;
+        nx = nn;
       }
-      if (more) {
-        address(Vp, nx, klo, khi);
-        tl.load_v(klo, khi);
-      }
-      p = nx;
-      nx = nn;
+      if (!fine) break;
+      float z[4] = {0.f, 0.f, 0.f, 0.f};                   // 0 times a number, or not a number
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) z[rr] = fmaf(o[i][rr], 0.f, z[rr]);
+      const bool bad = !((z[0] + z[1]) + (z[2] + z[3]) == 0.f);
+      if (!__any(bad)) break;
+      fine = false;
     }
     lrun = sum_across_quarters(lrun);
     // ---- the wavefronts' results together ------------------------------------------------------------------------------
+    int tid_ = tid;
+    asm volatile("" : "+v"(tid_));                         // (what follows from it is formed here, not kept in registers over the tiles)
+    const int n_ = tid_ & 15, kg_ = (tid_ & 63) >> 4;
 #pragma unroll
     for (int rr = 0; rr < 4; ++rr) {
-      const int head = 4 * kg + rr;
+      const int head = 4 * kg_ + rr;
       if (head < ng)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) sets[(wave * rows_max + head) * D + n * NV + i] = o[i][rr];
+        for (int i = 0; i < NV; ++i) sets[(wave * rows_max + head) * D + n_ * NV + i] = o[i][rr];
     }
-    if (lane < PD_HEADS) wml[wave][lane] = make_float2(mrun, lrun);
+    if ((tid_ & 63) < PD_HEADS) wml[wave][n_] = make_float2(mrun, lrun);
     __syncthreads();
     const bool whole = tile == 0 && t_end == sp.total;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (begun ? 1 : 0);
-    int tid_ = tid;
-    asm volatile("" : "+v"(tid_));                         // (what follows from it is formed here, not kept in registers over the tiles)
     for (int idx = tid_; idx < ng * (D / 4); idx += PD_THREADS) {
       const int head = idx / (D / 4), e = idx % (D / 4) * 4;
       float M = -INFINITY, L = 0.f;

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
         pr[j] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], c, -ref));
         lrun += pr[j];
       }
-      tl.add(pr, o);
+      tl.add(pr, o, true);
     }
     if (more) {
       address(Vp, nx, lo, hi);

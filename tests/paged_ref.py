@@ -61,12 +61,12 @@ def visible(pos, n_units, window, sink):
     return see
 
 
-def attend(q, K, V, see, scale, dtype):
+def attend(q, K, V, see, scale, dtype, factor=None):
     """One query q [d] over K, V [n][d] -> (out [d], lse, tolerance of out [d], tolerance of lse).
 
     Tolerance: a logit is a sum of d exact products in 32 bits, off by at most d 2^-24 of the sum of their sizes, then scaled and subtracted
     (2^-22 of its size in all); an exponential and the sums add some 2^-22.  So a probability is off by a relative `rel`,
-    twice with its normalisation, and where it becomes a 16-bit factor by STEP more; the output is rounded once."""
+    twice with its normalisation, and where it becomes a 16-bit factor by STEP more (`factor` instead, if given); the output is rounded once."""
     see = see.copy()
     if not see.any():
         return np.zeros(q.shape[0]), -math.inf, np.zeros(q.shape[0]), 0.0
@@ -80,7 +80,7 @@ def attend(q, K, V, see, scale, dtype):
         out = p @ V
         size = p @ np.abs(V)
         rel = 2 * (q.shape[0] * 2.0 ** -24 * scale * (np.abs(K) @ np.abs(q)).max() + 2.0 ** -22 * np.abs(s).max() + 2.0 ** -20)
-        half = STEP["bf16"] if dtype == "bf16" else 0.0
+        half = 0.0 if dtype == "f32" else STEP["bf16"] if factor is None else factor
         tol = size * (rel + half) + np.abs(out) * STEP[dtype] + 1e-30
     lse = top + math.log(total)
     return out, lse, tol, rel + 2.0 ** -22 * abs(lse)
