@@ -315,6 +315,27 @@ def test_decode_follows_its_definition(dtype, h, h_kv, d, page, lens, window, si
     close(lse, wl, ltol, "lse")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_as_many_requests_as_a_call_takes(dtype):
+    rng = np.random.default_rng(90)
+    n = B.LOCRET_PAGED_MAX_REQS
+    lens = rng.integers(0, 4, n).tolist()
+    lens[7] = 700
+    c = paged_case(rng, dtype, 16, 1, 128, 16, lens)
+    q, q64 = numbers(rng, dtype, n, 16, 128)
+    out, lse = run_decode(c, q)
+    want, wl, tol, ltol = reference_with_empty(c, q64)
+    close(out, want, tol, "decode")
+    close(lse, wl, ltol, "decode lse")
+    c = paged_case(rng, dtype, 2, 1, 32, 16, lens)
+    new = [int(rng.integers(0, x + 1)) for x in lens]
+    q, q64 = numbers(rng, dtype, sum(new), 2, 32)
+    out, lse = run_prefill(c, q, np.cumsum([0] + new))
+    want, wl, tol, ltol = reference(c, q64, new)
+    close(out, want, tol, "prefill")
+    close(lse, wl, ltol, "prefill lse")
+
+
 def reference_with_empty(c, q64):
     T, h, d = q64.shape
     some = [r for r, n in enumerate(c["lens"]) if n]
