@@ -104,16 +104,16 @@ __device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm,
   return true;
 }
 
-// The keys of an item: sink tiles from 0, then window tiles from wb, up to n_keys.
+// The keys of an item: sink tiles over [0, ns), then window tiles from wb, of which keys from w_lo on count (none of them a sink), up to n_keys.
+// (Tiles start at multiples of 16, or of their own length where a page holds one.)
 struct PfKeys {
   int n_keys, w_lo, ns, wb, ns_t, n_tiles;
 };
-// (Tiles start at multiples of 16, or of their own length where a page holds one.)
 __device__ __forceinline__ PfKeys pf_keys(const PfItem& it, const PagedDims& Dm, int KT) {
   PfKeys k;
   k.n_keys = max(it.p0 + it.n_tok, 0);                    // (positions below 0 see nothing)
-  k.w_lo = Dm.window ? max(0, it.p0 - Dm.window + 1) : 0;
-  k.ns = min(Dm.n_sink, k.w_lo);
+  k.ns = Dm.window ? min(Dm.n_sink, k.n_keys) : 0;
+  k.w_lo = Dm.window ? max(k.ns, it.p0 - Dm.window + 1) : 0;
   k.wb = k.w_lo & ~((1 << Dm.page_shift >= KT ? KT : 16) - 1);
   k.ns_t = (k.ns + KT - 1) / KT;
   k.n_tiles = k.ns_t + (max(k.n_keys - k.wb, 0) + KT - 1) / KT;
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   const int pos = it.p0 + tok;
   const int pw0 = it.p0 + min(wave * 32, rows - 1) / g, pw1 = it.p0 + min(wave * 32 + 31, rows - 1) / g;
   // first keys of the tiles that all rows of the wavefront see whole (among the sinks: up to all_sink), and of those that some row sees a key of
-  const int all_lo = Dm.window ? max(ks_.w_lo, pw1 - Dm.window + 1) : 0, all_hi = pw0 - KT + 1, all_sink = ks_.ns - KT;
+  const int all_lo = Dm.window ? max(ks_.w_lo, pw1 - Dm.window + 1) : 0, all_hi = pw0 - KT + 1, all_sink = min(ks_.ns - KT, all_hi);
   const int any_lo = Dm.window ? pw0 - Dm.window - KT + 2 : 0, any_hi = wave * 32 < rows ? pw1 : -1;
 
   bf16x8 qf[NKS];
@@ -320,12 +320,11 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     }
   };
 
-  // what the lane's row sees: key of tile t
-  auto sees = [&](int t, int key) __attribute__((always_inline)) {
-    bool s;
-    if (t < ks_.ns_t) s = key < ks_.ns && key <= pos;
-    else s = key >= ks_.w_lo && key <= pos && (Dm.window == 0 || pos - key < Dm.window || key < Dm.n_sink);
-    return s;
+  // what the lane's row sees of tile t: the keys from lo on, n of them
+  auto interval = [&](int t, int& lo, uint32_t& n) __attribute__((always_inline)) {
+    const bool sink = t < ks_.ns_t;
+    lo = sink || Dm.window == 0 ? 0 : max(ks_.w_lo, pos - Dm.window + 1);
+    n = max((sink ? min(ks_.ns, pos + 1) : pos + 1) - lo, 0);
   };
 
   // softmax and PV of tile t, whose logits are in sacc
@@ -334,21 +333,14 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     // does every row of the wavefront see the whole tile?
     const bool whole = t < ks_.ns_t ? kb0 <= all_sink : kb0 >= all_lo && kb0 <= all_hi;
     if (!whole) {
-      if (t >= ks_.ns_t && kb0 < Dm.n_sink) {  // sinks and window may lie apart in this tile
+      int lo;
+      uint32_t n;
+      interval(t, lo, n);
+      const int x = lo - kb0 - hi * 4;
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb)
+      for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!sees(t, kb0 + kb * 32 + (r >> 2) * 8 + hi * 4 + (r & 3))) sacc[kb][r] = -INFINITY;
-      } else {                                 // the row sees the keys from lo on, n of them
-        const int lo = t < ks_.ns_t ? 0 : Dm.window ? max(ks_.w_lo, pos - Dm.window + 1) : 0;
-        const uint32_t n = max((t < ks_.ns_t ? ks_.ns : pos + 1) - lo, 0);
-        const int x = lo - kb0 - hi * 4;
-#pragma unroll
-        for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[kb][r] = (uint32_t)(kb * 32 + (r >> 2) * 8 + (r & 3) - x) < n ? sacc[kb][r] : -INFINITY;
-      }
+        for (int r = 0; r < 16; ++r) sacc[kb][r] = (uint32_t)(kb * 32 + (r >> 2) * 8 + (r & 3) - x) < n ? sacc[kb][r] : -INFINITY;
     }
     uint32_t pw[NKB * 8];                      // probabilities, two keys a word
     float ps;
@@ -432,7 +424,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   // does some row of the wavefront see some key of tile t?
   auto active = [&](int t) __attribute__((always_inline)) {
     const int kb = tile_key(t);
-    return kb <= any_hi && (t < ks_.ns_t || kb >= any_lo || kb < Dm.n_sink);
+    return kb <= any_hi && (t < ks_.ns_t || kb >= any_lo);
   };
   if (wave >= PF_NW / 2) {
     issue(0);
@@ -497,6 +489,9 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
 #pragma unroll 1
     for (int t = t_lo; t < t_hi; ++t) {
       if (!active(t)) continue;
+      int lo;
+      uint32_t n;
+      interval(t, lo, n);
       const int kb0 = tile_key(t), end = min(t < ks_.ns_t ? ks_.ns : ks_.n_keys, kb0 + KT);
 #pragma unroll 1
       for (int key = kb0; key < end; ++key) {
@@ -510,7 +505,7 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
 #pragma unroll
           for (int r = 0; r < 16; ++r) s = fmaf(qv[db][r], bf2f(kr[db * 32 + (r >> 2) * 8 + (r & 3)]), s);
         s += __shfl_xor(s, 32, 64);
-        const bool see = sees(t, key);
+        const bool see = (uint32_t)(key - lo) < n;
         const float x = see ? s * c : -INFINITY, m_new = fmaxf(m_run, x), ref = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(m_run - ref), p = __builtin_amdgcn_exp2f(x - ref);
         l = l * alpha + p;

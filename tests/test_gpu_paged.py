@@ -700,6 +700,47 @@ def test_calls_on_another_stream():
     np.testing.assert_array_equal(host(out), want[0])
 
 
+def test_calls_at_once_with_a_workspace_each():
+    """Decode and prefill on two streams together, many times, against the same calls one after the other."""
+    rng = np.random.default_rng(43)
+    c = paged_case(rng, "bf16", 8, 2, 128, 16, [3000, 900, 40])
+    q, _ = numbers(rng, "bf16", 90, 8, 128)
+    table, lens, cu = ints(c["table"]), ints(c["lens"]), ints([0, 40, 75, 90])
+    ws = [workspace(c["cfg"]) for _ in range(2)]
+    outs = [[torch.zeros_like(q) for _ in range(2)] for _ in range(2)]
+
+    def call(i, o):
+        if i == 0:
+            B.locret_paged_decode(c["cfg"], 3, q[:3], c["K"], c["V"], table, lens, o[:3], None, ws[0])
+        else:
+            B.locret_paged_prefill(c["cfg"], 3, 90, q, c["K"], c["V"], table, lens, cu, o, None, ws[1])
+
+    for i in range(2):
+        call(i, outs[0][i])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                call(i, outs[1][i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(outs[0][i], outs[1][i])
+
+
+def test_the_same_request_twice_in_a_batch():
+    """Two rows of the block table with the same pages (a shared prompt)."""
+    rng = np.random.default_rng(44)
+    c = paged_case(rng, "bf16", 8, 2, 64, 32, [500, 500, 100], 200, 4)
+    c["table"][1] = c["table"][0]
+    q, q64 = numbers(rng, "bf16", 60, 8, 64)
+    new = [25, 25, 10]
+    out, lse = run_prefill(c, q, np.cumsum([0] + new))
+    want, wl, tol, ltol = reference(c, q64, new)
+    close(out, want, tol, "prefill")
+    close(lse, wl, ltol, "prefill lse")
+
+
 def test_results_do_not_depend_on_what_the_workspace_held():
     rng = np.random.default_rng(42)
     c = paged_case(rng, "bf16", 4, 1, 128, 16, [9000, 500])
