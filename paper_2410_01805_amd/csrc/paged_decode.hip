@@ -42,7 +42,7 @@ __device__ __forceinline__ PagedSpan paged_span(int n, int window, int n_sink) {
   return s;
 }
 
-// Units a workgroup takes.  (Divisions of 64 bits take a microsecond; sums of units that need them are rare.)
+// Units a workgroup takes.  (Divisions of 64 bits are a hundred instructions in front of the first load; sums of units that need them are rare.)
 __device__ __forceinline__ int64_t units_per_wg(int64_t all, int n_wg) {
   if (all < (int64_t)1 << 30) return ((uint32_t)all + n_wg - 1) / (uint32_t)n_wg;
   return (all + n_wg - 1) / n_wg;

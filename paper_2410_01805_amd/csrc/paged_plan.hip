@@ -21,7 +21,7 @@ struct PlanSmem {
   int len[PAGED_MAX_REQS];          // units before the step (0 where the request is finished)
   int cu[PAGED_MAX_REQS + 1];       // N_r
   int want[PAGED_MAX_REQS + 1];     // W_r
-  uint32_t part[3 * PLAN_MAX_THREADS / 64];
+  uint32_t part[4 * PLAN_MAX_THREADS / 64];
 };
 
 __device__ __forceinline__ int pages_of(int units, int shift) { return (int)(((int64_t)units + (1 << shift) - 1) >> shift); }
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(PLAN_MAX_THREADS) void plan_kernel(PagedPlan p, int
   const int tid = threadIdx.x, nt = blockDim.x;
   const int most = p.max_pages << p.page_shift;
   int len[PLAN_IPT], add[PLAN_IPT], held[PLAN_IPT];    // add: tokens asked for, -1 finished
-  uint32_t mine[3] = {0, 0, 0}, before[3], all[3];     // pages given back, pages wanted, tokens
+  uint32_t mine[4] = {0, 0, 0, 0}, before[4], all[4];  // pages given back, pages wanted, tokens; requests that give back
 #pragma unroll
   for (int u = 0; u < PLAN_IPT; ++u) {
     const int r = tid * ipt + u;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(PLAN_MAX_THREADS) void plan_kernel(PagedPlan p, int
       len[u] = min(max(p.lens[r], 0), most);
       add[u] = p.n_new[r];
       held[u] = pages_of(len[u], p.page_shift);
-      if (add[u] < 0) { add[u] = -1; mine[0] = add_sat(mine[0], held[u]); }
+      if (add[u] < 0) { add[u] = -1; mine[0] = add_sat(mine[0], held[u]); mine[3] += held[u] > 0; }
       else if (add[u] > most - len[u]) add[u] = 0;
       if (add[u] > 0) {
         mine[1] = add_sat(mine[1], pages_of(len[u] + add[u], p.page_shift) - held[u]);
@@ -81,24 +81,32 @@ __global__ __launch_bounds__(PLAN_MAX_THREADS) void plan_kernel(PagedPlan p, int
     }
   }
   const int n_free = min(max(p.n_free[0], 0), p.n_pages);
-  block_exclusive<3>(mine, before, all, s.part);
+  block_exclusive<4>(mine, before, all, s.part);
   const int n_all_free = (int)min(add_sat(n_free, all[0]), (uint32_t)p.n_pages);
   if (all[0] > 0) {
-    // pages of finished requests: s.want and s.len hold B_r and the lengths meanwhile
-    uint32_t b = before[0];
+    // s.cu and s.want hold the requests that give pages back, and B_r, meanwhile.  A wavefront takes 256 pages: one bisection, four loads on their
+    // way together (26 requests of 12.7 thousand pages 5.4 us; with a bisection over all requests for every page 10).
+    uint32_t b = before[0], k = before[3];
 #pragma unroll
-    for (int u = 0; u < PLAN_IPT; ++u) {
-      const int r = tid * ipt + u;
-      if (u < ipt && r < p.n_req) {
-        s.want[r] = (int)min(b, (uint32_t)INT32_MAX);
-        if (add[u] < 0) b = add_sat(b, held[u]);
+    for (int u = 0; u < PLAN_IPT; ++u)
+      if (add[u] < 0 && held[u] > 0) {
+        s.cu[k] = tid * ipt + u;
+        s.want[k++] = (int)min(b, (uint32_t)INT32_MAX);
+        b = add_sat(b, held[u]);
       }
-    }
     __syncthreads();
-#pragma unroll 4
-    for (int i = tid; i < n_all_free - n_free; i += nt) {
-      const int r = last_at_or_before(s.want, p.n_req, i);
-      p.free_pages[n_free + i] = p.table[(int64_t)r * p.max_pages + (i - s.want[r])];
+    const int n = n_all_free - n_free, n_back = (int)all[3];
+    for (int i0 = (tid >> 6) * 256; i0 < n; i0 += nt * 4) {
+      int j = last_at_or_before(s.want, n_back, i0), id[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = min(i0 + e * 64 + (tid & 63), n - 1);
+        while (j + 1 < n_back && s.want[j + 1] <= i) ++j;
+        id[e] = p.table[(int64_t)s.cu[j] * p.max_pages + (i - s.want[j])];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (i0 + e * 64 + (tid & 63) < n) p.free_pages[n_free + i0 + e * 64 + (tid & 63)] = id[e];
     }
     __syncthreads();
   }

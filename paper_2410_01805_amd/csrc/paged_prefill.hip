@@ -14,8 +14,8 @@
 //
 // Tiles (64 keys of 128 or 96 dims, 128 of 64 or 32) come from the pages to a ring of 4 stages in LDS without passing through registers: a
 // load instruction of a wavefront covers 1 KB of LDS, which is 4 or 8 keys and lies inside 16 keys that start at a multiple of 16, so it
-// lies inside one page of any size, and has a descriptor of its own: base = those keys in the page, length = how many of them are
-// there.  What is behind the last key, on no page, or padding of a row arrives as zeros.  LDS rows have 256 bytes (keys of 64 or 32 dims lie two
+// lies inside one page of any size.  Its descriptor has those keys in the page as base and how many of them are there as length; where a page
+// holds whole tiles, one serves the whole tile.  What is behind the last key, on no page, or padding of a row arrives as zeros.  LDS rows have 256 bytes (keys of 64 or 32 dims lie two
 // in a row); position c' of row r holds the 16-byte chunk c' ^ f(r), with f chosen so that neither the fragment reads of K nor the
 // transposing ones of V meet in a bank: f = r mod 16 for K; 4 (r mod 4), or 4 (r mod 2) with two keys in a row, for V.
 // At X(t) tiles t and t+1 are in LDS, and every wavefront is done with t-1, whose stage the loads of t+3 overwrite.
@@ -29,7 +29,7 @@
 // the keys that each row sees.  (There no tile's registers are alive; the same inside the loop took half of its speed in spills, and looking
 // through the values of masked tiles a third of the time of 12 ragged requests with a window, 94 -> 59 us.)
 //
-// Few rows: where the items (tokens tile, KV head) are at most half as many as the CUs, each one's keys are cut into parts,
+// Few rows: where the items (token tile, KV head) are at most half as many as the CUs, each one's keys are cut into parts,
 // workgroups of their own, which leave maximum, sum and accumulators; a second launch joins them.
 #include "attn_common.h"
 #include "paged.h"
