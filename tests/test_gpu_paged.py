@@ -315,6 +315,22 @@ def test_decode_follows_its_definition(dtype, h, h_kv, d, page, lens, window, si
     close(lse, wl, ltol, "lse")
 
 
+@pytest.mark.parametrize("n", [63, 64, 65, 128])
+@pytest.mark.parametrize("ends", [0, 300])
+def test_decode_of_about_a_wavefront_of_requests(n, ends):
+    rng = np.random.default_rng(n + ends)
+    lens = rng.integers(0, 200, n).tolist()
+    lens[0] = lens[1] = lens[-2] = lens[-1] = ends
+    lens[20] = lens[21] = 0
+    lens[40] = 3000
+    c = paged_case(rng, "bf16", 8, 2, 64, 16, lens, window=900, sink=3)
+    q, q64 = numbers(rng, "bf16", n, 8, 64)
+    out, lse = run_decode(c, q)
+    want, wl, tol, ltol = reference_with_empty(c, q64)
+    close(out, want, tol, "out")
+    close(lse, wl, ltol, "lse")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_as_many_requests_as_a_call_takes(dtype):
     rng = np.random.default_rng(90)
