@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 # PyTorch ships its own HIP runtime (soname libamdhip64.so.7).  It must be in the process before
 # liblocret.so is opened so that the dynamic loader binds the library to that same runtime:
@@ -110,7 +111,7 @@ def _load() -> C.CDLL:
     lib.locret_rope_frequencies.restype = C.c_int
     lib.locret_rope_frequencies.argtypes = [C.POINTER(locret_rope_config), C.POINTER(C.c_double), C.POINTER(C.c_float)]
     lib.locret_paged_append.restype = C.c_int
-    lib.locret_paged_append.argtypes = [cfg, i32, vp, vp, vp, C.POINTER(C.c_int64), vp, vp, vp, i32, i32, C.c_float, vp, vp,
+    lib.locret_paged_append.argtypes = [cfg, i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, C.c_float, vp, vp,
                                         C.c_float, vp, vp, vp, vp]
     lib.locret_paged_decode.restype = C.c_int
     lib.locret_paged_decode.argtypes = [cfg, i32] + [vp] * 8 + [C.c_size_t, vp]
@@ -349,6 +350,9 @@ def locret_rope_frequencies(rotary_dim, theta, scaling=LOCRET_ROPE_PLAIN, factor
     return list(freq), amplitude.value
 
 
+_strides = struct.Struct("6q").pack                        # (0.1 us; an array of c_int64 takes 0.9)
+
+
 def _paged_rows(where, dev, t, dtype, T, heads, d, st, i):
     """Address of q, k or v [T][heads][d] with any strides between tokens and heads, which go to st[i], st[i + 1]."""
     if t is None or t.__class__ is int:
@@ -356,9 +360,14 @@ def _paged_rows(where, dev, t, dtype, T, heads, d, st, i):
     if t.dtype is not dtype or t.get_device() != dev:
         raise LocretError(LOCRET_EINVAL, where)
     shape = t.shape
-    if len(shape) != 3 or shape[0] < T or shape[1] != heads or shape[2] != d or t.stride(2) != 1:
+    if len(shape) != 3:
         raise LocretError(LOCRET_ESHAPE, where)
-    st[i], st[i + 1] = t.stride(0), t.stride(1)
+    n, a, b = shape
+    s0, s1, s2 = t.stride()
+    if n < T or a != heads or b != d or s2 != 1:
+        raise LocretError(LOCRET_ESHAPE, where)
+    st[i] = s0
+    st[i + 1] = s1
     return t.data_ptr()
 
 
@@ -369,14 +378,11 @@ def locret_paged_append(cfg, T, q, k, v, positions, slots, freq, rotary_dim, int
     h, m, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     pool, dtype = cfg.n_pages * m * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
     dev = _paged_device(w, q, K)
-    if strides is None:
-        st = (C.c_int64 * 6)(h * d, d, m * d, d, m * d, d)
-    elif len(strides) == 6:
-        st = (C.c_int64 * 6)(*strides)
-    else:
+    st = [h * d, d, m * d, d, m * d, d] if strides is None else list(strides)
+    if len(st) != 6:
         raise LocretError(LOCRET_EINVAL, w)
     args = (C.byref(cfg), T, _paged_rows(w, dev, q, dtype, T, h, d, st, 0), _paged_rows(w, dev, k, dtype, T, m, d, st, 2),
-            _paged_rows(w, dev, v, dtype, T, m, d, st, 4), st, _paged_ptr(w, dev, positions, torch.int32, T),
+            _paged_rows(w, dev, v, dtype, T, m, d, st, 4), _strides(*st), _paged_ptr(w, dev, positions, torch.int32, T),
             _paged_ptr(w, dev, slots, torch.int32, T), _paged_ptr(w, dev, freq, torch.float64, rotary_dim // 2), rotary_dim,
             1 if interleaved else 0, amplitude, _paged_ptr(w, dev, q_weight, f32, d), _paged_ptr(w, dev, k_weight, f32, d), eps,
             _paged_ptr(w, dev, q_out, dtype, T * h * d), _paged_ptr(w, dev, K, dtype, pool), _paged_ptr(w, dev, V, dtype, pool))
