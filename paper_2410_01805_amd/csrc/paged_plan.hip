@@ -34,7 +34,8 @@ __device__ __forceinline__ void plan_fill(const PagedPlan& p, const PlanSmem& s,
     const int r = last_at_or_before(s.want, p.n_req, i);
     p.table[(int64_t)r * p.max_pages + pages_of(s.len[r], p.page_shift) + (i - s.want[r])] = p.free_pages[n_all_free - 1 - i];
   }
-  for (int t = t0; t < t1; t += 4 * blockDim.x) {
+  const int t_step = 4 * (int)blockDim.x;
+  for (int t = t0; t < t1; t = t1 - t > t_step ? t + t_step : t1) {      // (max_tokens may be the largest number)
     int slot[4], pos[4], r = t < total ? last_at_or_before(s.cu, p.n_req, t) : 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {

@@ -129,6 +129,20 @@ def test_plan_without_requests():
     assert nf.item() == 4
 
 
+def test_plan_with_the_largest_number_of_tokens():
+    most = 2 ** 31 - 1
+    cfg = config(n_pages=6, max_pages=3, max_reqs=2)
+    slots, pos = torch.full((most,), 3, **I32), torch.full((most,), 3, **I32)
+    cu, nf2, out = ints([9] * 3), ints([0]), ints([0, 0])
+    B.locret_paged_plan(cfg, 2, ints([0, 17]), ints([20, 3]), out, ints([[-1, -1, -1], [4, 5, -1]]), ints([0, 1, 2, 3, 9, 9]), ints([4]), nf2, most, cu, slots, pos)
+    assert nf2.item() == 2 and cu.tolist() == [0, 20, 23] and out.tolist() == [20, 20]
+    assert slots[:23].tolist() == [48 + i for i in range(16)] + [32 + i for i in range(4)] + [80 + i for i in range(1, 4)]
+    assert pos[:23].tolist() == list(range(20)) + [17, 18, 19]
+    assert slots[23:].max().item() == slots[23:].min().item() == -1 and pos[23:].max().item() == pos[23:].min().item() == 0
+    del slots, pos
+    torch.cuda.empty_cache()
+
+
 # ---- append ----------------------------------------------------------------------------------------------------------
 APPEND = [
     # dtype, h, h_kv, d, T, rot, interleaved, norm, page, strided
