@@ -11,7 +11,7 @@ struct PagedDims {
   int page_shift;       // log2 of the page size
   int n_pages;
   int max_pages;
-  int window, n_sink;   // window 0: none
+  int window, n_sink;   // window 0: none; else less than the units of a row
   float scale;
 };
 
@@ -83,6 +83,10 @@ typedef const __attribute__((address_space(4))) int32_t* paged_const_i32;
 __device__ __forceinline__ int paged_len(const int32_t* lens, int r, int max_pages, int page_shift) {
   return min(max(lens[r], 0), max_pages << page_shift);
 }
+
+// A position as the kernels compare it.  A chunk may be up to T tokens longer than its request: those in front of the first unit see nothing, at -1 as
+// far below it, from where a window's first key is still a number of 32 bits.
+__device__ __forceinline__ int paged_pos(int p) { return max(p, -1); }
 
 __device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 

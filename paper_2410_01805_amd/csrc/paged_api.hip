@@ -34,7 +34,8 @@ int validate(const locret_paged_config* c, PagedDims* D) {
   D->page_shift = shift;
   D->n_pages = c->n_pages;
   D->max_pages = c->max_pages;
-  D->window = c->window;
+  // a window that reaches over a whole row hides nothing; the others are below 2^30, so that position - window stays in 32 bits
+  D->window = (int64_t)c->window >= (int64_t)c->max_pages << shift ? 0 : c->window;
   D->n_sink = c->n_sink;
   D->scale = c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)c->head_dim);
   return LOCRET_OK;

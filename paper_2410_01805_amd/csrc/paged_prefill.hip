@@ -113,7 +113,7 @@ __device__ __forceinline__ PfKeys pf_keys(const PfItem& it, const PagedDims& Dm,
   PfKeys k;
   k.n_keys = max(it.p0 + it.n_tok, 0);                    // (positions below 0 see nothing)
   k.ns = Dm.window ? min(Dm.n_sink, k.n_keys) : 0;
-  k.w_lo = Dm.window ? max(k.ns, it.p0 - Dm.window + 1) : 0;
+  k.w_lo = Dm.window ? max(k.ns, paged_pos(it.p0) - Dm.window + 1) : 0;
   k.wb = k.w_lo & ~((1 << Dm.page_shift >= KT ? KT : 16) - 1);
   k.ns_t = (k.ns + KT - 1) / KT;
   k.n_tiles = k.ns_t + (max(k.n_keys - k.wb, 0) + KT - 1) / KT;
@@ -164,8 +164,8 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
   // this lane's row, and the first and last position of the wavefront's
   const int row = min(wave * 32 + n32, rows - 1), tok = row / g;
   const int64_t at = (int64_t)(it.t0 + tok) * Dm.h + it.m * g + (row - tok * g);
-  const int pos = it.p0 + tok;
-  const int pw0 = it.p0 + min(wave * 32, rows - 1) / g, pw1 = it.p0 + min(wave * 32 + 31, rows - 1) / g;
+  const int pos = paged_pos(it.p0 + tok);
+  const int pw0 = paged_pos(it.p0 + min(wave * 32, rows - 1) / g), pw1 = paged_pos(it.p0 + min(wave * 32 + 31, rows - 1) / g);
   // first keys of the tiles that all rows of the wavefront see whole (among the sinks: up to all_sink), and of those that some row sees a key of
   const int all_lo = Dm.window ? max(ks_.w_lo, pw1 - Dm.window + 1) : 0, all_hi = pw0 - KT + 1, all_sink = min(ks_.ns - KT, all_hi);
   const int any_lo = Dm.window ? pw0 - Dm.window - KT + 2 : 0, any_hi = wave * 32 < rows ? pw1 : -1;

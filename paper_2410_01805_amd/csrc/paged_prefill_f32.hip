@@ -63,8 +63,8 @@ struct PrSpan {
 };
 __device__ __forceinline__ PrSpan pr_span(const PrItem& it, const PagedDims& Dm) {
   PrSpan s;
-  const int p0 = it.pos0 + it.row0 / Dm.g, p1 = it.pos0 + (it.row0 + it.n_rows - 1) / Dm.g;
-  s.end = max(p1 + 1, 0);
+  const int p0 = paged_pos(it.pos0 + it.row0 / Dm.g), p1 = paged_pos(it.pos0 + (it.row0 + it.n_rows - 1) / Dm.g);
+  s.end = p1 + 1;
   s.w0 = Dm.window ? max(0, p0 - Dm.window + 1) : 0;
   s.ns = min(Dm.n_sink, s.w0);
   s.wb = s.w0 & ~31;
@@ -103,9 +103,9 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
   const float* Kp = (const float*)a.K + (int64_t)it.m * page * D;
   const float* Vp = (const float*)a.V + (int64_t)it.m * page * D;
   // this lane's row (a column of S^T): spare ones repeat the last
-  const int row = it.row0 + min(n, it.n_rows - 1), tok = row / Dm.g, pos = it.pos0 + tok;
+  const int row = it.row0 + min(n, it.n_rows - 1), tok = row / Dm.g, pos = paged_pos(it.pos0 + tok);
   const int64_t at = (int64_t)(it.t0 + tok) * Dm.h + it.m * Dm.g + (row - tok * Dm.g);
-  const int pmin = it.pos0 + it.row0 / Dm.g;
+  const int pmin = paged_pos(it.pos0 + it.row0 / Dm.g);
   const float c = Dm.scale * 1.4426950408889634f;
   auto sees = [&](bool sink, int key) __attribute__((always_inline)) {
     if (sink) return key < sp.ns && key <= pos;

@@ -786,3 +786,48 @@ def test_results_do_not_depend_on_what_the_workspace_held():
             call(o, ws)
             outs.append(o)
         assert torch.equal(*outs)
+
+
+# ---- the ends of what a call takes -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("bf16", 96, 16), ("bf16", 64, 128), ("bf16", 32, 16), ("f32", 64, 16)])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 120, 2 ** 30, "row", "row - 1"])
+@pytest.mark.parametrize("sink", [0, 5, 2 ** 31 - 1])
+def test_windows_longer_than_the_requests(dtype, d, page, window, sink):
+    """Windows up to the largest number, as long as a row of the block table and one less: all units up to a token's own are seen."""
+    rng = np.random.default_rng(d + page)
+    lens, new = [200, 3, 90, 1], [200, 3, 20, 1]
+    c = paged_case(rng, dtype, 8, 2, d, page, lens)
+    row = c["cfg"].max_pages * page
+    c["cfg"].window = {"row": row, "row - 1": row - 1}.get(window, window)
+    c["cfg"].n_sink = sink
+    q, q64 = numbers(rng, dtype, sum(new), 8, d)
+    cu = np.cumsum([0] + new)
+    out, lse = run_prefill(c, q, cu)
+    want, wl, tol, ltol = reference(c, q64, new)
+    close(out, want, tol, "prefill")
+    close(lse, wl, ltol, "prefill lse")
+    last = cu[1:] - 1
+    out, lse = run_decode(c, q[torch.from_numpy(last).to(DEV)].contiguous())
+    want, wl, tol, ltol = reference(c, q64[last], [1] * 4, DECODE_FACTOR)
+    close(out, want, tol, "decode")
+    close(lse, wl, ltol, "decode lse")
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("window", [0, 1, 20, 2 ** 31 - 1])
+@pytest.mark.parametrize("sink", [0, 3, 2 ** 31 - 1])
+def test_chunks_longer_than_their_requests(dtype, d, window, sink):
+    """Tokens in front of a request's first unit see nothing, with windows and sinks of any size; the others see what they do elsewhere."""
+    rng = np.random.default_rng(d + 1)
+    lens, new = [5, 70, 0, 33], [40, 70, 6, 300]
+    c = paged_case(rng, dtype, 8, 2, d, 16, lens, window, sink)
+    q, q64 = numbers(rng, dtype, sum(new), 8, d)
+    cu = np.cumsum([0] + new)
+    out, lse = run_prefill(c, q, cu)
+    some = [min(k, n) for k, n in zip(new, lens)]          # the last ones of each
+    there = np.concatenate([np.arange(cu[r + 1] - k, cu[r + 1]) for r, k in enumerate(some)])
+    want, wl, tol, ltol = reference(c, q64[there], some)
+    close(out[there], want, tol, "out")
+    close(lse[there], wl, ltol, "lse")
+    rest = np.setdiff1d(np.arange(sum(new)), there)
+    assert (out[rest] == 0).all() and np.isneginf(lse[rest]).all()
