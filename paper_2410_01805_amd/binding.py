@@ -584,7 +584,8 @@ class PagedCache:
 
     def adopt(self, layer: "LocretLayer", r: int) -> None:
         """The retained cache of `layer` (its heads equally long, rows not packed) becomes the next units of request r, which generation
-        then continues: on an empty request, unit i sits at position i here as there."""
+        then continues: on an empty request, unit i sits at position i here as there.  Waits for the device: where the request's row of
+        the block table is too short (LOCRET_ESHAPE) or too few pages are free (LOCRET_ENOMEM) the pool stays as it was."""
         c, n = layer.cfg, layer.cache_len
         if (c.n_kv_heads, c.head_dim, c.dtype) != (self.cfg.n_kv_heads, self.cfg.head_dim, self.cfg.dtype) or not 0 <= r < self.cfg.max_reqs:
             raise LocretError(LOCRET_ESHAPE, "adopt")
@@ -592,7 +593,10 @@ class PagedCache:
             raise LocretError(LOCRET_ESTATE, "adopt")
         n_new = torch.zeros(r + 1, dtype=torch.int32, device=self.device)
         n_new[r] = n
-        _, slots, positions = self.plan(n_new, n)
+        cu_new, slots, positions = self.plan(n_new, n)
+        if cu_new[-1].item() != n:
+            row = self.cfg.max_pages * self.cfg.page_size
+            raise LocretError(LOCRET_ESHAPE if self.lens[r].item() + n > row else LOCRET_ENOMEM, "adopt")
         view = locret_cache_view(layer.ctx)
         row, d = view["row_stride"], c.head_dim
         locret_paged_append(self.cfg, n, None, view["K"], view["V"], positions, slots, self.freq, self.rotary_dim, self.interleaved, self.amplitude,

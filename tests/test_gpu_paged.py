@@ -831,3 +831,51 @@ def test_chunks_longer_than_their_requests(dtype, d, window, sink):
     close(lse[there], wl, ltol, "lse")
     rest = np.setdiff1d(np.arange(sum(new)), there)
     assert (out[rest] == 0).all() and np.isneginf(lse[rest]).all()
+
+
+# ---- adopting what a context retained --------------------------------------------------------------------------------
+def retained(n=150, budget=90):
+    """A context that has evicted to its budget."""
+    w = synth.tiny(name="adopted", dtype="bf16", h=8, h_kv=2, d=64, N=n, B=50, b=budget, n_s=10, d_R=128, rope=True, theta=10000.0)
+    layer, _, _ = make_layer(w)
+    for lo in range(0, w.N, w.B):
+        layer.prefill_chunk(*(dev(x, w) for x in synth.tokens(w, lo, min(w.N, lo + w.B))), w.n_s)
+    return layer
+
+
+@pytest.mark.parametrize("n_pages,max_pages,taken,code", [
+    (5, 16, 0, B.LOCRET_ENOMEM),      # 90 units are 6 pages of 16
+    (8, 16, 37, B.LOCRET_ENOMEM),     # 3 pages belong to another request
+    (20, 5, 0, B.LOCRET_ESHAPE),      # a row holds 80 units
+    (3, 5, 0, B.LOCRET_ESHAPE),       # both
+])
+def test_adopt_refuses_what_the_pool_cannot_hold(n_pages, max_pages, taken, code):
+    """An error, a pool that stays as it was, and one that goes on to be used."""
+    layer = retained()
+    assert layer.cache_len == 90
+    cache = B.PagedCache(config("bf16", 8, 2, 64, 16, n_pages, 3, max_pages), DEV, rope=dict(rotary_dim=64, theta=10000.0))
+    cache.K.fill_(3.0)
+    cache.V.fill_(4.0)
+    if taken:
+        cache.plan(ints([taken]), taken)
+    state = lambda: [x.clone() for x in (cache.K, cache.V, cache.block_table, cache.lens, cache.free_pages, cache.n_free)]
+    before = state()
+    with pytest.raises(B.LocretError) as e:
+        cache.adopt(layer, 1)
+    assert e.value.code == code
+    assert all(torch.equal(a, b) for a, b in zip(before, state()))
+    cu, slots, _ = cache.plan(ints([0, 20]), 20)
+    assert cu.tolist() == [0, 0, 20] and (slots >= 0).all()
+
+
+def test_adopt_behind_units_that_fill_the_row_to_its_end():
+    layer = retained()
+    cache = B.PagedCache(config("bf16", 8, 2, 64, 16, 40, 2, 7), DEV, rope=dict(rotary_dim=64, theta=10000.0))
+    cache.plan(ints([0, 22]), 22)                          # 22 + 90 units: the row's 112
+    cache.adopt(layer, 1)
+    assert cache.lens.tolist() == [0, 112] and cache.n_free.item() == 33
+    with pytest.raises(B.LocretError) as e:
+        cache.adopt(layer, 1)
+    assert e.value.code == B.LOCRET_ESHAPE and cache.lens.tolist() == [0, 112] and cache.n_free.item() == 33
+    cache.adopt(layer, 0)
+    assert cache.lens.tolist() == [90, 112]
