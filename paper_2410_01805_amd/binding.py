@@ -544,6 +544,7 @@ class PagedCache:
         ints = dict(dtype=torch.int32, device=self.device)
         pool = (cfg.n_pages, cfg.n_kv_heads, cfg.page_size, cfg.head_dim)
         self.K, self.V = torch.empty(pool, dtype=self.tdtype, device=self.device), torch.empty(pool, dtype=self.tdtype, device=self.device)
+        self.device = ints["device"] = self.K.device       # with its number, also where none was given
         self.block_table = torch.zeros((cfg.max_reqs, cfg.max_pages), **ints)
         self.lens = torch.zeros(cfg.max_reqs, **ints)
         self.free_pages = torch.arange(cfg.n_pages - 1, -1, -1, **ints)
@@ -589,7 +590,7 @@ class PagedCache:
         c, n = layer.cfg, layer.cache_len
         if (c.n_kv_heads, c.head_dim, c.dtype) != (self.cfg.n_kv_heads, self.cfg.head_dim, self.cfg.dtype) or not 0 <= r < self.cfg.max_reqs:
             raise LocretError(LOCRET_ESHAPE, "adopt")
-        if c.kv_bits or len(set(layer.cache_lens)) != 1 or layer.device != self.device:
+        if c.kv_bits or len(set(layer.cache_lens)) != 1 or layer.workspace.device != self.device:
             raise LocretError(LOCRET_ESTATE, "adopt")
         n_new = torch.zeros(r + 1, dtype=torch.int32, device=self.device)
         n_new[r] = n

@@ -879,3 +879,16 @@ def test_adopt_behind_units_that_fill_the_row_to_its_end():
     assert e.value.code == B.LOCRET_ESHAPE and cache.lens.tolist() == [0, 112] and cache.n_free.item() == 33
     cache.adopt(layer, 0)
     assert cache.lens.tolist() == [90, 112]
+
+
+def test_adopt_of_a_context_on_a_device_without_a_number():
+    """"cuda" is the current device, for the pool and for the context."""
+    layer = retained()
+    cache = B.PagedCache(config("bf16", 8, 2, 64, 16, 20, 2, 16), "cuda", rope=dict(rotary_dim=64, theta=10000.0))
+    cache.adopt(layer, 0)
+    other = B.LocretLayer(layer.cfg, "cuda")
+    other.set_weights(*(torch.zeros(s, dtype=torch.bfloat16, device=DEV) for s in ((12 * 64, 128), (128, 2))))
+    x = torch.randn(10, 12, 64, device=DEV).bfloat16()
+    other.prefill_chunk(x[:, :8].contiguous(), x[:, 8:10].contiguous(), x[:, 10:].contiguous(), 1)
+    cache.adopt(other, 1)
+    assert cache.lens.tolist() == [90, 10]
