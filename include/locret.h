@@ -327,7 +327,7 @@ int locret_rope_frequencies(const locret_rope_config* cfg, double* freq, float* 
  * All in 32 bits, rounded once.  Slots of a call are distinct; tokens whose slot is outside the pool (-1: padding) leave their query only.
  * rotary_dim  0 (freq and positions are not read) or a multiple of 16, at most head_dim
  * strides     HOST, NULL for dense tensors, or elements between tokens and between heads: {q token, q head, k token, k head, v token,
- *             v head}, at least 0 and multiples of 16 bytes
+ *             v head}, at least 0 and multiples of 16 bytes; one between tokens is not looked at if T = 1, between heads if there is one
  * q and q_out may be NULL together, k and v (and slots, K, V) too.  q_out may be q where q is dense. */
 int locret_paged_append(const locret_paged_config* cfg, int32_t T, const void* q, const void* k, const void* v, const int64_t* strides,
                         const int32_t* positions, const int32_t* slots, const double* freq, int32_t rotary_dim,

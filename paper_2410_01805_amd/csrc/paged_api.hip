@@ -144,12 +144,14 @@ int locret_paged_append(const locret_paged_config* cfg, int32_t T, const void* q
   const int64_t d = D.d, dense[6] = {D.h * d, d, D.h_kv * d, d, D.h_kv * d, d};
   const int64_t* s = strides ? strides : dense;
   const int vec = D.bf16 ? 8 : 4;
+  // a stride that leads nowhere, of one token or one head, may be anything
+  auto used = [&](int i) { return i & 1 ? (i < 2 ? D.h : D.h_kv) > 1 : T > 1; };
   for (int i = 0; i < 6; ++i) {
-    if (!(i < 2 ? q : k)) continue;
+    if (!(i < 2 ? q : k) || !used(i)) continue;
     if (s[i] < 0) return LOCRET_EINVAL;
     if (s[i] % vec) return LOCRET_EALIGN;
   }
-  if (q && q_out == q && (s[0] != dense[0] || s[1] != dense[1])) return LOCRET_EINVAL;
+  for (int i = 0; i < 2; ++i) if (q && q_out == q && used(i) && s[i] != dense[i]) return LOCRET_EINVAL;
   const void* p[] = {q, k, v, q_out, K, V, q_weight, k_weight};
   for (const void* x : p) if (misaligned(x)) return LOCRET_EALIGN;
   if (misaligned(positions, 4) || misaligned(slots, 4) || misaligned(freq, 8)) return LOCRET_EALIGN;

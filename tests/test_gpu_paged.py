@@ -892,3 +892,48 @@ def test_adopt_of_a_context_on_a_device_without_a_number():
     other.prefill_chunk(x[:, :8].contiguous(), x[:, 8:10].contiguous(), x[:, 10:].contiguous(), 1)
     cache.adopt(other, 1)
     assert cache.lens.tolist() == [90, 10]
+
+
+# ---- strides that lead nowhere ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_of_one_token_of_a_fused_product(dtype):
+    """In place on one token's slice, which is dense whatever its token stride, and with a token stride that no vector load could take."""
+    rng = np.random.default_rng(61)
+    h, h_kv, d = 8, 2, 64
+    cfg = config(dtype, h, h_kv, d, 16, 4)
+    pos, slots = ints([77]), ints([21])
+    freq = torch.tensor(B.locret_rope_frequencies(d, 10000.0)[0], dtype=torch.float64, device=DEV)
+    x, _ = numbers(rng, dtype, 1, h + 2 * h_kv, d)
+    want, K, V, K2, V2 = (torch.zeros(s, dtype=tt(dtype), device=DEV) for s in ((1, h, d), *((4, h_kv, 16, d),) * 4))
+    parts = lambda y: (y[:, :h], y[:, h: h + h_kv], y[:, h + h_kv:])
+    B.locret_paged_append(cfg, 1, *(y.contiguous() for y in parts(x)), pos, slots, freq, d, False, 1.0, None, None, 0.0, want, K, V)
+    for stride in (12 * d, 7, 0):
+        y = x.clone()
+        q, k, v = (z.as_strided((1, z.shape[1], d), (stride, d, 1)) for z in parts(y))
+        B.locret_paged_append(cfg, 1, q, k, v, pos, slots, freq, d, False, 1.0, None, None, 0.0, q, K2, V2)
+        assert torch.equal(q, want) and torch.equal(K, K2) and torch.equal(V, V2), stride
+        assert torch.equal(y[:, h:], x[:, h:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_of_one_head(dtype):
+    rng = np.random.default_rng(62)
+    T, d = 9, 32
+    cfg = config(dtype, 1, 1, d, 16, 4)
+    pos, slots = ints(range(T)), ints(range(5, 5 + T))
+    freq = torch.tensor(B.locret_rope_frequencies(d, 10000.0)[0], dtype=torch.float64, device=DEV)
+    x, _ = numbers(rng, dtype, T, 3, d)
+    want, got, K, V, K2, V2 = (torch.zeros(s, dtype=tt(dtype), device=DEV) for s in (*((T, 1, d),) * 2, *((4, 1, 16, d),) * 4))
+    q, k, v = (x[:, i: i + 1] for i in range(3))
+    B.locret_paged_append(cfg, T, q.contiguous(), k.contiguous(), v.contiguous(), pos, slots, freq, d, False, 1.0, None, None, 0.0, want, K, V)
+    q, k, v = (y.as_strided((T, 1, d), (3 * d, 1, 1)) for y in (q, k, v))
+    B.locret_paged_append(cfg, T, q, k, v, pos, slots, freq, d, False, 1.0, None, None, 0.0, got, K2, V2)
+    assert torch.equal(got, want) and torch.equal(K, K2) and torch.equal(V, V2)
+    q = q.contiguous()                                     # in place, where the head stride is no more looked at
+    B.locret_paged_append(cfg, T, q.data_ptr(), None, None, pos.data_ptr(), None, freq.data_ptr(), d, False, 1.0, None, None, 0.0, q.data_ptr(), None, None,
+                          strides=[d, 5, 0, 0, 0, 0])
+    assert torch.equal(q, want)
+    with pytest.raises(B.LocretError) as e:                # the token stride is
+        B.locret_paged_append(cfg, T, q.data_ptr(), None, None, pos.data_ptr(), None, freq.data_ptr(), d, False, 1.0, None, None, 0.0, q.data_ptr(), None, None,
+                              strides=[2 * d, d, 0, 0, 0, 0])
+    assert e.value.code == B.LOCRET_EINVAL
