@@ -293,7 +293,7 @@ def _paged_ptr(where, dev, t, dtype, numel):
 
 
 def _paged_device(where, *tensors) -> int:
-    """Index of the device of the first tensor; -1 (the current device) if all are addresses."""
+    """Index of the device of the first tensor among a call's arguments; -1 (the current device) if all are addresses."""
     for t in tensors:
         if t is not None and t.__class__ is not int:
             dev = t.get_device()
@@ -329,7 +329,7 @@ def locret_paged_workspace_bytes(cfg: locret_paged_config) -> int:
 def locret_paged_plan(cfg, n_req, lens, n_new, lens_out, block_table, free_pages, n_free, n_free_out, max_tokens, cu_new, slots, positions,
                       stream=None) -> None:
     w, i32 = "locret_paged_plan", torch.int32
-    dev = _paged_device(w, cu_new, free_pages)
+    dev = _paged_device(w, cu_new, free_pages, lens, n_new, lens_out, block_table, n_free, n_free_out, slots, positions)
     args = (C.byref(cfg), n_req, _paged_ptr(w, dev, lens, i32, n_req), _paged_ptr(w, dev, n_new, i32, n_req),
             _paged_ptr(w, dev, lens_out, i32, n_req), _paged_ptr(w, dev, block_table, i32, n_req * cfg.max_pages),
             _paged_ptr(w, dev, free_pages, i32, cfg.n_pages), _paged_ptr(w, dev, n_free, i32, 1), _paged_ptr(w, dev, n_free_out, i32, 1),
@@ -377,7 +377,7 @@ def locret_paged_append(cfg, T, q, k, v, positions, slots, freq, rotary_dim, int
     w, f32 = "locret_paged_append", torch.float32
     h, m, d = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
     pool, dtype = cfg.n_pages * m * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
-    dev = _paged_device(w, q, K)
+    dev = _paged_device(w, q, K, k, v, positions, slots, freq, q_weight, k_weight, q_out, V)
     st = [h * d, d, m * d, d, m * d, d] if strides is None else list(strides)
     if len(st) != 6:
         raise LocretError(LOCRET_EINVAL, w)
@@ -393,7 +393,7 @@ def locret_paged_decode(cfg, n_req, q, K, V, block_table, lens, out, lse, worksp
     w, i32 = "locret_paged_decode", torch.int32
     h, d = cfg.n_q_heads, cfg.head_dim
     n, pool, dtype = n_req * h * d, cfg.n_pages * cfg.n_kv_heads * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
-    dev = _paged_device(w, q, K, block_table)
+    dev = _paged_device(w, q, K, V, block_table, lens, out, lse, workspace)
     if workspace_bytes is None:
         workspace_bytes = workspace.nbytes if torch.is_tensor(workspace) else 0
     args = (C.byref(cfg), n_req, _paged_ptr(w, dev, q, dtype, n), _paged_ptr(w, dev, K, dtype, pool), _paged_ptr(w, dev, V, dtype, pool),
@@ -406,7 +406,7 @@ def locret_paged_prefill(cfg, n_req, T, q, K, V, block_table, lens, cu_new, out,
     w, i32 = "locret_paged_prefill", torch.int32
     h, d = cfg.n_q_heads, cfg.head_dim
     n, pool, dtype = T * h * d, cfg.n_pages * cfg.n_kv_heads * cfg.page_size * d, _PAGED_DTYPE.get(cfg.dtype)
-    dev = _paged_device(w, q, K, block_table)
+    dev = _paged_device(w, q, K, V, block_table, lens, cu_new, out, lse, workspace)
     if workspace_bytes is None:
         workspace_bytes = workspace.nbytes if torch.is_tensor(workspace) else 0
     args = (C.byref(cfg), n_req, T, _paged_ptr(w, dev, q, dtype, n), _paged_ptr(w, dev, K, dtype, pool), _paged_ptr(w, dev, V, dtype, pool),

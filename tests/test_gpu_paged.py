@@ -937,3 +937,49 @@ def test_append_of_one_head(dtype):
         B.locret_paged_append(cfg, T, q.data_ptr(), None, None, pos.data_ptr(), None, freq.data_ptr(), d, False, 1.0, None, None, 0.0, q.data_ptr(), None, None,
                               strides=[2 * d, d, 0, 0, 0, 0])
     assert e.value.code == B.LOCRET_EINVAL
+
+
+def test_addresses_and_tensors_in_one_call():
+    """Any argument may be an address beside tensors; results are those of tensors alone."""
+    rng = np.random.default_rng(63)
+    c = paged_case(rng, "bf16", 8, 2, 64, 16, [70, 33])
+    q, _ = numbers(rng, "bf16", 20, 8, 64)
+    table, lens, cu, ws = ints(c["table"]), ints(c["lens"]), ints([0, 12, 20]), workspace(c["cfg"])
+    calls = {
+        "decode": lambda o, l, f: B.locret_paged_decode(c["cfg"], 2, *(f(i, x) for i, x in enumerate((q, c["K"], c["V"], table, lens, o, l, ws))),
+                                                        workspace_bytes=ws.nbytes),
+        "prefill": lambda o, l, f: B.locret_paged_prefill(c["cfg"], 2, 20, *(f(i, x) for i, x in enumerate((q, c["K"], c["V"], table, lens, cu, o, l, ws))),
+                                                          workspace_bytes=ws.nbytes),
+    }
+    for what, call in calls.items():
+        n = 2 if what == "decode" else 20
+        mk = lambda: (torch.zeros(n, 8, 64, dtype=torch.bfloat16, device=DEV), torch.zeros(n, 8, device=DEV))
+        want, got = mk(), mk()
+        call(*want, lambda i, x: x)
+        for keep in range(8):                              # one tensor left
+            for x in got:
+                x.zero_()
+            call(*got, lambda i, x: x if i == keep else x.data_ptr())
+            assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1]), (what, keep)
+    x, _ = numbers(rng, "bf16", 5, 12, 64)
+    k, v, pos, slots = x[:, 8:10].contiguous(), x[:, 10:].contiguous(), ints(range(5)), ints(range(3, 8))
+    want, got = torch.empty_like(q[:5]), torch.empty_like(q[:5])
+    freq = torch.tensor(B.locret_rope_frequencies(64, 10000.0)[0], dtype=torch.float64, device=DEV)
+    pools = [torch.zeros_like(c["K"]) for _ in range(4)]
+    args = lambda o, K, V: (q[:5], k, v, pos, slots, freq, o, K, V)
+    call = lambda a: B.locret_paged_append(c["cfg"], 5, *a[:6], 64, False, 1.0, None, None, 0.0, *a[6:])
+    call(args(want, *pools[:2]))
+    for keep in range(9):
+        got.zero_(), pools[2].zero_(), pools[3].zero_()
+        call([x if i == keep else x.data_ptr() for i, x in enumerate(args(got, *pools[2:]))])
+        assert torch.equal(want, got) and torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3]), keep
+    state = lambda: [ints([5, 17]), ints([20, 3]), ints([0, 0]), ints([[4, -1, -1], [2, 3, -1]]), ints([0, 1, 5, 6, 9, 9, 9]), ints([4]), ints([0]), ints([9] * 3),
+                     torch.zeros(30, **I32), torch.zeros(30, **I32)]
+    cfg = config(n_pages=7, max_pages=3, max_reqs=2)
+    call = lambda a: B.locret_paged_plan(cfg, 2, *a[:7], 30, *a[7:])
+    want = state()
+    call(want)
+    for keep in range(10):
+        got = state()
+        call([x if i == keep else x.data_ptr() for i, x in enumerate(got)])
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), keep
