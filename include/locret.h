@@ -264,7 +264,10 @@ int locret_profile_read(locret_ctx* ctx, double* stage_ms, int32_t* n_calls);
  *   - device data is bounded by the kernels: lengths are taken as at least 0 and at most max_pages * page_size, units of a
  *     block-table entry outside 0 .. n_pages - 1 are not seen, slots outside the pool are not written.
  *   - attention: what a query does not see does not reach its result, whatever is stored there (infinities and NaN included).
- *     Values that are seen may be up to 2^64 in size before their sums can leave the range of float. */
+ *     Values that are seen may be up to 2^64 in size before their sums can leave the range of float.
+ *   - attention: a key whose logit is -inf (infinities in keys or queries) has weight 0, and a row that sees no other keys is
+ *     answered like one that sees nothing: zeros and lse -inf.  Whether a value that is not finite reaches the result of other rows
+ *     through a weight of 0 is not defined.  Logits of +inf or NaN give NaN. */
 typedef struct {
   int32_t n_q_heads;      /* h; h / n_kv_heads at most 128                                       */
   int32_t n_kv_heads;     /* must divide n_q_heads                                               */

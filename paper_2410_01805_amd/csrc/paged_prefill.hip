@@ -519,6 +519,11 @@ __global__ __launch_bounds__(PF_THREADS, 2) void paged_prefill_kernel(PagedAttn 
     }
     if (m_run == -INFINITY) m_run = 0.f;
     l_run = hi ? 0.f : l;
+    if (l == 0.f)                              // only logits of -inf: 0, also where a value of weight 0 is not finite
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
   }
 
   // ---- results ---------------------------------------------------------------------------------------------------------

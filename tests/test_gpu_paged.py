@@ -983,3 +983,42 @@ def test_addresses_and_tensors_in_one_call():
         got = state()
         call([x if i == keep else x.data_ptr() for i, x in enumerate(got)])
         assert all(torch.equal(a, b) for a, b in zip(want, got)), keep
+
+
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("bf16", 64, 16), ("f32", 64, 16), ("f32", 96, 32)])
+@pytest.mark.parametrize("window,sink", [(0, 0), (50, 4)])
+@pytest.mark.parametrize("value", [None, float("inf"), float("nan")])
+def test_rows_whose_logits_are_all_minus_infinity(dtype, d, page, window, sink, value):
+    """Keys of -inf weigh nothing: rows that see only such are zeros and -inf, whatever their values hold, the others are what is left of theirs."""
+    rng = np.random.default_rng(d + page + window)
+    lens, new = [700, 200, 90], [30, 200, 90]
+    c = paged_case(rng, dtype, 4, 2, d, page, lens, window, sink)
+    gone = [np.zeros(n, dtype=bool) for n in lens]
+    gone[0][:] = True                                      # all of them
+    gone[1][:120] = True                                   # rows up to 119, and later ones whose window starts with them
+    for r, g in enumerate(gone):
+        for u in np.flatnonzero(g):
+            p, i = c["table"][r, u // page], u % page
+            c["K"][p, :, i, 0] = -math.inf
+            if value is not None and r == 0 and u % 3 == 0:
+                c["V"][p, :, i, :: 5] = value
+    q, q64 = numbers(rng, dtype, sum(new), 4, d)
+    q[..., 0] = 1.0
+    q64[..., 0] = 1.0
+    cu = np.cumsum([0] + new)
+
+    def check(rows, out, lse, what):
+        want, wl, tol, ltol = (np.zeros((len(rows),) + s) for s in ((4, d), (4,), (4, d), (4,)))
+        for t, (r, i) in enumerate(rows):
+            for j in range(4):
+                see = R.visible(lens[r] - new[r] + i, lens[r], window, sink) & ~gone[r]
+                K, V = (units(c, c[x], r, j // 2)[0] for x in ("K64", "V64"))
+                want[t, j], wl[t, j], tol[t, j], ltol[t, j] = R.attend(q64[cu[r] + i, j], K, V, see, c["scale"], dtype)
+        close(out, want, tol, what)
+        close(lse, wl, ltol, what + " lse")
+
+    out, lse = run_prefill(c, q, cu)
+    check([(r, i) for r in range(3) for i in range(new[r])], out, lse, "prefill")
+    assert (out[:30] == 0).all() and (out[30: 150] == 0).all() and np.isneginf(lse[:150]).all()
+    out, lse = run_decode(c, q[torch.from_numpy(cu[1:] - 1).to(DEV)].contiguous())
+    check([(r, new[r] - 1) for r in range(3)], out, lse, "decode")
