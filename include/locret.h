@@ -269,7 +269,7 @@ int locret_profile_read(locret_ctx* ctx, double* stage_ms, int32_t* n_calls);
  *     answered like one that sees nothing: zeros and lse -inf.  Whether a value that is not finite reaches the result of other rows
  *     through a weight of 0 is not defined.  Logits of +inf or NaN give NaN. */
 typedef struct {
-  int32_t n_q_heads;      /* h; h / n_kv_heads at most 128                                       */
+  int32_t n_q_heads;      /* h, at most 1024; h / n_kv_heads at most 128                         */
   int32_t n_kv_heads;     /* must divide n_q_heads                                               */
   int32_t head_dim;       /* 32, 64, 96 or 128                                                   */
   int32_t dtype;          /* LOCRET_F32 or LOCRET_BF16: type of q, k, v, out and the pool        */
@@ -347,8 +347,8 @@ int locret_paged_decode(const locret_paged_config* cfg, int32_t n_req, const voi
 /* Causal attention of a ragged batch of chunks.  Request r's queries are tokens cu_new[r] .. cu_new[r+1] - 1 of q
  * [T][n_q_heads][head_dim] and the last of its lens[r] units (already appended): token cu_new[r] + i stands at position
  * lens[r] - (cu_new[r+1] - cu_new[r]) + i and sees the units up to there, in the window or among the sinks.  cu_new does not fall and
- * is taken within 0 .. T.  Rows of out and lse (as above) that belong to no request stay as they were; rows that see
- * nothing are zeros and -inf. */
+ * is taken within 0 .. T.  T * n_q_heads is at most 2^34, for float 2^31 (LOCRET_ESHAPE).  Rows of out and lse (as above) that belong
+ * to no request stay as they were; rows that see nothing are zeros and -inf. */
 int locret_paged_prefill(const locret_paged_config* cfg, int32_t n_req, int32_t T, const void* q, const void* K, const void* V,
                          const int32_t* block_table, const int32_t* lens, const int32_t* cu_new, void* out, float* lse,
                          void* workspace, size_t workspace_bytes, void* stream);

@@ -53,7 +53,8 @@ int attention(const locret_paged_config* cfg, const PagedAttn& a, size_t bytes, 
   const int rc = validate(cfg, &D);
   if (rc != LOCRET_OK) return rc;
   if (a.n_req < 0 || a.T < 0) return LOCRET_EINVAL;
-  if (a.n_req > cfg->max_reqs || (int64_t)a.T * D.h > (int64_t)1 << 34) return LOCRET_ESHAPE;      // (launches are counted in 32 bits)
+  // (launches are counted in 32 bits, the float prefill's rows of a request too)
+  if (a.n_req > cfg->max_reqs || (int64_t)a.T * D.h > (int64_t)1 << (D.bf16 ? 34 : 31)) return LOCRET_ESHAPE;
   if (a.n_req == 0 || a.T == 0) return LOCRET_OK;
   if (!a.q || !a.K || !a.V || !a.table || !a.lens || (prefill && !a.cu) || !a.out || !a.ws) return LOCRET_EINVAL;
   if (misaligned(a.q) || misaligned(a.K) || misaligned(a.V) || misaligned(a.out) || misaligned(a.ws, 256) || misaligned(a.table, 4) ||

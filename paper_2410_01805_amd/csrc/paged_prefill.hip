@@ -69,7 +69,7 @@ __device__ __forceinline__ bool pf_item(const PagedAttn& a, const PagedDims& Dm,
     const int r = tid * ipt + u;
     if (r < a.n_req) {
       const int c0 = paged_cu(a.cu, r, a.T), n = max(paged_cu(a.cu, r + 1, a.T) - c0, 0);
-      first[r + 1] = (n + tw - 1) / tw;
+      first[r + 1] = (int)(((uint32_t)n + tw - 1) / tw);      // (n may be the largest number)
       mine += first[r + 1];
     }
   }

@@ -188,3 +188,16 @@ def test_frequencies_refuse(kw, code):
     with pytest.raises(B.LocretError) as e:
         B.locret_rope_frequencies(**{**dict(rotary_dim=64, theta=10000.0), **kw})
     assert e.value.code == code
+
+
+@pytest.mark.parametrize("dtype,most", [(B.LOCRET_F32, 1 << 31), (B.LOCRET_BF16, 1 << 34)])
+@pytest.mark.parametrize("h", [16, 1024])
+def test_prefill_takes_rows_up_to_its_limit(dtype, most, h):
+    c = cfg(n_q_heads=h, n_kv_heads=h // 16, dtype=dtype)
+    assert prefill(c, T=most // h, bytes_=0) == ENOMEM     # (the workspace is looked at behind the sizes)
+    assert prefill(c, T=most // h + 1) == ESHAPE
+
+
+def test_layouts_of_up_to_1024_heads():
+    assert B.locret_paged_workspace_bytes(cfg(n_q_heads=1024, n_kv_heads=8)) > 0
+    assert B.locret_paged_workspace_bytes(cfg(n_q_heads=1032, n_kv_heads=129)) == 0
