@@ -249,8 +249,8 @@ int locret_profile_read(locret_ctx* ctx, double* stage_ms, int32_t* n_calls);
  *                 ceil(length / page_size) on are never read
  *   lens          [n_req] int32: units of every request in the cache
  *   slot          page * page_size + place in the page, of one unit
- * A serving step is locret_paged_plan, then for every layer locret_paged_append and locret_paged_decode (one new token a
- * request) or locret_paged_prefill (ragged chunks).  The retained cache of a locret_ctx is moved into pages by
+ * A serving step is locret_paged_plan, then for every layer locret_paged_append and locret_paged_decode (every request has one new
+ * token) or locret_paged_prefill (any other step: chunks, requests that wait or are finished).  The retained cache of a locret_ctx is moved into pages by
  * locret_paged_append too: its K and V (locret_cache_view) are read with head strides, rotated to positions 0, 1, ...
  *
  * Conventions: those of the top of this file, except
@@ -339,7 +339,11 @@ int locret_paged_append(const locret_paged_config* cfg, int32_t T, const void* q
 
 /* Attention of one token per request, the last of its lens[r] units (already appended):
  * q, out [n_req][n_q_heads][head_dim]; lse float [n_req][n_q_heads] or NULL: log of the sum of the exponentials of the visible
- * logits.  A request that sees nothing (length 0) gets zeros and lse -inf. */
+ * logits.  A request that sees nothing (length 0) gets zeros and lse -inf.
+ * Rows are requests, not the packed tokens of a step: the two are the same only where every request was given one token, cu_new[r] = r.  Where
+ * one waits, is finished or was given nothing, tokens behind it stand in lower rows than their requests: such a step goes through
+ * locret_paged_prefill, which reads cu_new, or row r of q is filled from token cu_new[r] (rows of the others have to be there; what
+ * comes out for them means nothing). */
 int locret_paged_decode(const locret_paged_config* cfg, int32_t n_req, const void* q, const void* K, const void* V,
                         const int32_t* block_table, const int32_t* lens, void* out, float* lse, void* workspace,
                         size_t workspace_bytes, void* stream);

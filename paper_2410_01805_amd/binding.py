@@ -533,7 +533,8 @@ class PagedCache:
     """Owns one layer's pool of pages, its bookkeeping and a workspace; methods forward to the C ABI (no arithmetic here).
 
     A serving step: plan() gives the new tokens' places, append() brings their queries, keys and values there, decode() (one new token for each
-    of the first n_req requests) or prefill() (ragged chunks) attends.  `rope`: arguments of locret_rope_frequencies, None for no rotation."""
+    of the first n_req requests, row r of q is that of request r) or prefill() (any other step: chunks, requests that wait or are finished,
+    whose packed tokens it finds by cu_new) attends.  `rope`: arguments of locret_rope_frequencies, None for no rotation."""
 
     def __init__(self, cfg: locret_paged_config, device="cuda:0", rope=None, interleaved=False):
         self.cfg, self.device = cfg, torch.device(device)

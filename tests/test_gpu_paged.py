@@ -1022,3 +1022,38 @@ def test_rows_whose_logits_are_all_minus_infinity(dtype, d, page, window, sink, 
     assert (out[:30] == 0).all() and (out[30: 150] == 0).all() and np.isneginf(lse[:150]).all()
     out, lse = run_decode(c, q[torch.from_numpy(cu[1:] - 1).to(DEV)].contiguous())
     check([(r, new[r] - 1) for r in range(3)], out, lse, "decode")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_step_in_which_requests_wait_finish_or_are_not_served(dtype):
+    """One token each for the others: packed rows through prefill, rows by request through decode, against the definition."""
+    h, h_kv, d, page = 8, 2, 64, 16
+    rng = np.random.default_rng(71)
+    cache = B.PagedCache(config(dtype, h, h_kv, d, page, n_pages=20, max_reqs=6, max_pages=5), DEV)
+    streams = [[np.zeros((0, n, d)) for n in (h, h_kv, h_kv)] for _ in range(6)]
+    # request 1 waits, 3 is finished; in the last step the row of 4 is too short and there is no page left for 5
+    for new in ([33, 50, 0, 20, 64, 48], [1, 0, 1, -1, 1, 1], [10, 0, 40, 5, 30, 20]):
+        T = sum(max(n, 0) for n in new)
+        x, x64 = numbers(rng, dtype, T, h + 2 * h_kv, d)
+        cu, slots, pos = cache.plan(ints(new), T)
+        q = cache.append(x[:, :h], x[:, h: h + h_kv], x[:, h + h_kv:], pos, slots)
+        at = cu.tolist()
+        for r, n in enumerate(new):
+            if n < 0:
+                streams[r] = [y[:0] for y in streams[r]]
+            for i, (lo, hi) in enumerate(((0, h), (h, h + h_kv), (h + h_kv, h + 2 * h_kv))):
+                streams[r][i] = np.concatenate([streams[r][i], x64[at[r]: at[r + 1], lo: hi]])
+        assert cache.lens.tolist() == [s[0].shape[0] for s in streams]
+        out = host(cache.prefill(q, cu))
+        rows = torch.zeros(6, h, d, dtype=q.dtype, device=DEV)
+        last = [at[r + 1] - 1 for r in range(6)]
+        has = [r for r in range(6) if at[r + 1] > at[r]]
+        rows[has] = q[[last[r] for r in has]]
+        dec = host(cache.decode(rows))
+        for r in has:
+            n = at[r + 1] - at[r]
+            want, tol = dense_reference(streams[r], [], 0, (None, None), n, 0, 0, dtype, h // h_kv)
+            close(out[at[r]: at[r + 1]], want, tol, f"prefill of request {r} of {new}")
+            close(dec[r: r + 1], want[-1:], tol[-1:], f"decode of request {r} of {new}")
+        assert (dec[[r for r in range(6) if not streams[r][0].shape[0]]] == 0).all()
+    assert at == [0, 10, 10, 50, 55, 55, 55]
