@@ -107,9 +107,17 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
   const int64_t at = (int64_t)(it.t0 + tok) * Dm.h + it.m * Dm.g + (row - tok * Dm.g);
   const int pmin = paged_pos(it.pos0 + it.row0 / Dm.g);
   const float c = Dm.scale * 1.4426950408889634f;
-  auto sees = [&](bool sink, int key) __attribute__((always_inline)) {
-    if (sink) return key < sp.ns && key <= pos;
-    return key >= sp.w0 && key <= pos && (Dm.window == 0 || pos - key < Dm.window || key < Dm.n_sink);
+  // what the row sees of a tile: the keys [lo, hi), and behind the sinks' tiles the sinks [w0, s1) too
+  struct Seen { int lo, hi, s1; };
+  auto seen_of = [&](bool sink) __attribute__((always_inline)) {
+    Seen v;
+    v.lo = sink || Dm.window == 0 ? 0 : max(sp.w0, pos - Dm.window + 1);
+    v.hi = sink ? min(sp.ns, pos + 1) : pos + 1;
+    v.s1 = sink ? 0 : min(Dm.n_sink, pos + 1);
+    return v;
+  };
+  auto sees = [&](const Seen& v, int key) __attribute__((always_inline)) {
+    return ((key >= v.lo) & (key < v.hi)) | ((key >= sp.w0) & (key < v.s1));
   };
   struct Place { bool sink; int kb, end, id0, id1; };
   auto place = [&](int u) __attribute__((always_inline)) {
@@ -170,13 +178,10 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
         const int id = kg >= 2 ? p.id1 : p.id0, k0 = p.kb + 8 * kg;
         const uint32_t there = (unsigned)id < (unsigned)Dm.n_pages ? (1u << min(max(p.end - k0, 0), 8)) - 1u : 0u;
         tl.clear_v(there);
-        // and the row sees the keys [lo, hi), and sinks that are not in front of the window's first tile
-        const int lo = sink || Dm.window == 0 ? 0 : max(sp.w0, pos - Dm.window + 1), hi = sink ? min(sp.ns, pos + 1) : pos + 1;
-        const int s1 = sink ? 0 : min(Dm.n_sink, pos + 1);
+        const Seen v = seen_of(sink);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int key = k0 + j;
-          const bool see = ((there >> j) & 1) & (int)(((key >= lo) & (key < hi)) | ((key >= sp.w0) & (key < s1)));
+          const bool see = ((there >> j) & 1) & (int)sees(v, k0 + j);
           s[j >> 2][j & 3] = see ? s[j >> 2][j & 3] : -INFINITY;
         }
       }
@@ -230,6 +235,7 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
 #pragma unroll 1
     for (int u = u0; u < u1; ++u) {
       const Place w = place(u);
+      const Seen v = seen_of(w.sink);
 #pragma unroll 1
       for (int key = w.kb; key < min(w.end, w.kb + 32); ++key) {
         const int id = trow[key >> shift];
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(PR_THREADS, D >= 96 ? 2 : 3) void paged_prefill_f32
 #pragma unroll
         for (int e = 0; e < D / 4; ++e) s = fmaf(qv[e], Kp[off + e], s);
         s = sum_across_quarters(s);
-        const bool see = sees(w.sink, key);
+        const bool see = sees(v, key);
         const float x = see ? s * c : -INFINITY, m_new = fmaxf(mrun, x), ref = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(mrun - ref), pk = __builtin_amdgcn_exp2f(x - ref);
         l = l * alpha + pk;
