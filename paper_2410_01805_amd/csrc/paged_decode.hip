@@ -24,8 +24,8 @@ constexpr int PD_THREADS = 256, PD_NW = 4, PD_HEADS = 16;
 constexpr float PD_RESCALE_LOG2 = 8.f;
 
 // Workgroups a CU: what registers allow without spilling.
-template <typename T, int D> struct PagedOcc { static constexpr int value = sizeof(T) == 2 ? (D >= 96 ? 3 : 4) : (D >= 96 ? 2 : 3); };
-static int paged_decode_workgroups(const PagedDims& D) { return 256 * (D.bf16 ? (D.d >= 96 ? 3 : 4) : (D.d >= 96 ? 2 : 3)); }
+__host__ __device__ constexpr int paged_decode_occupancy(bool bf16, int d) { return bf16 ? (d >= 96 ? 3 : 4) : (d >= 96 ? 2 : 3); }
+static int paged_decode_workgroups(const PagedDims& D) { return 256 * paged_decode_occupancy(D.bf16, D.d); }
 
 // The visible keys of a request in tiles of 32: sinks, then from the first tile with a key in the window on; four tiles are a unit.
 struct PagedSpan {
@@ -90,7 +90,7 @@ size_t paged_decode_workspace(const PagedDims& D, int max_reqs) {
 }
 
 template <typename T, int D, bool SMALL>
-__global__ __launch_bounds__(PD_THREADS, (PagedOcc<T, D>::value)) void paged_decode_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm,
+__global__ __launch_bounds__(PD_THREADS, paged_decode_occupancy(sizeof(T) == 2, D)) void paged_decode_kernel(PagedAttn a, const int32_t* __restrict__ table, PagedDims Dm,
                                                                                            int passes, int ipt) {
   typedef typename PagedTileOf<T, D, SMALL>::type Tile;
   constexpr int NV = D / 16;
