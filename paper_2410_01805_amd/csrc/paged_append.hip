@@ -7,8 +7,8 @@
 // 16-byte chunks of a row, the partners of a rotation where the pairs are (i, i + rot/2), neighbours otherwise, so that
 // neither the rotation nor an update in place needs another lane's data.  A workgroup has one token (8192 tokens of 32 query and 8 KV heads of
 // 128 dims: 40.2 us, 5.0 TB/s, what a large copy reaches; with 2, 4, 8 tokens 41.9, 43.7, 44.7), whose angles it forms once, in LDS, for all
-// heads: the turns position * f / 2 pi in 64 bits, of which only the fraction goes on in 32 (a product in 32 bits would be off by
-// half a radian at position 2^20 with 2^-24 of rounding).
+// heads: the turns position * f / 2 pi in 64 bits, of which only the fraction goes on in 32 (a product in 32 bits is
+// rounded by up to 2^-24 of it, at position 2^20 by 2^-4 radians; the fraction is rounded by 2^-25 turns, 2^-22 radians).
 #include "device_util.h"
 #include "paged.h"
 

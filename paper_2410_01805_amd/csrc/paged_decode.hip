@@ -4,8 +4,8 @@
 // the heads of a group (16 at a time) as one side of a 16 x 16 tile, so that the arithmetic stays far below that bound for any group.
 //
 // Work: an item is (request, KV head, 16 query heads), a unit four tiles of 32 keys of an item (one a wavefront).  Lengths are known on the device only, and
-// differ, so the units of all items are laid end to end and every workgroup takes the same number of them, as many workgroups
-// as the chip holds at once.  Each workgroup forms the sums of units over the requests by itself (at most 4096 numbers from L2, one scan) and
+// differ, so the units of all items are laid end to end and every workgroup takes the same number of them, rounded up, as many workgroups
+// as the chip holds at once (with a unit or two for each the last ones have none: 1032 units are two each for 516 of 768).  Each workgroup forms the sums of units over the requests by itself (at most 4096 numbers from L2, one scan) and
 // finds its first unit by bisection.  An item that one workgroup holds whole is written by it; of one that is cut, every
 // workgroup leaves maximum, sum and sum of values (two such pieces a workgroup at most), and the second launch, which has a workgroup
 // per request and head, joins them in the order of the keys.  Results depend on no order of execution.

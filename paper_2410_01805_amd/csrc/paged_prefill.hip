@@ -22,15 +22,19 @@
 //
 // Softmax: logits stay unscaled in the accumulators and become exponents by one multiply-add (queries scaled before the product would have
 // to be rounded again, which costs the outputs twice the error).  The running maximum of a row is that of the first tile in which it sees
-// a key, and raised when the row's sum over a tile reaches 2^30.  Probabilities become bf16 factors, half a step of 2^-8 each; sums, maxima
-// and accumulators are 32-bit.
+// a key, and raised when the row's sum over a tile reaches 2^30.  Probabilities become one bf16 factor each, off by at most 2^-8 of themselves,
+// which with the outputs' own rounding of the same size makes these 1.41 times as far off as that rounding alone; two factors, as in the decode
+// kernel, would be half as many matrix instructions more (4096 tokens on 16384 units 841 -> 1170 us, 512 on 16384 136 -> 182, 12 ragged
+// requests with a window 77 -> 101).  Sums, maxima and accumulators are 32-bit.
 // Tiles that some row of a wavefront does not see whole are masked before the maximum.  A masked probability is 0, but 0 times a value that is
 // not finite is not: where an accumulator is not finite in the end, the wavefront forms its rows once more behind the loop, key by key, from
 // the keys that each row sees.  (There no tile's registers are alive; the same inside the loop took half of its speed in spills, and looking
 // through the values of masked tiles a third of the time of 12 ragged requests with a window, 94 -> 59 us.)
 //
 // Few rows: where the items (token tile, KV head) are at most half as many as the CUs, each one's keys are cut into parts,
-// workgroups of their own, which leave maximum, sum and accumulators; a second launch joins them.
+// workgroups of their own, which leave maximum, sum and accumulators; a second launch joins them.  (32 heads, 8 KV heads of 128 dims, us: 512 tokens
+// on 4096 units, 64 items in 4 parts 48.5, whole 99, in 8 parts 65.5; 1024 on 8192, 128 items in 2 parts 135, whole 190, in 4 144;
+// 1536 on 8192, 192 items whole 201, in 2 parts 212.)
 #include "attn_common.h"
 #include "paged.h"
 
@@ -44,8 +48,12 @@ typedef short pf_s16x8 __attribute__((ext_vector_type(8)));
 constexpr int PF_NW = 8, PF_THREADS = PF_NW * 64, PF_ROWS = PF_NW * 32;
 constexpr int PF_TILE_B = 64 * 256, PF_STAGE_B = 2 * PF_TILE_B;
 constexpr int PF_KPRE = 4;                     // K fragments fetched ahead of the S block
+// Parts of an item at most: the joining workgroups go over them one after the other.  (8 items: 16 tokens on 16384 units in 8, 16, 32 parts 51.4, 42.6,
+// 56.6 us; on 131072 units 280, 170, 141)
 constexpr int PF_CUS = 256, PF_MAX_PARTS = 16, PF_MAX_SLOTS = PF_CUS;
-constexpr int PF_MIN_PART = 4;                 // key tiles of a part at least: less does not pay for a part's prologue and joining
+// Key tiles of a part at least: fewer do not pay for a part's prologue and joining, more leave CUs idle.  (64 tokens on 700 units with 1, 2, 4, 8 tiles 20.5,
+// 18.6, 19.3, 24.2 us, on 1500 units 23.0, 22.8, 21.7, 25.0)
+constexpr int PF_MIN_PART = 4;
 
 // What a workgroup works on.
 struct PfItem {

@@ -201,3 +201,11 @@ def test_prefill_takes_rows_up_to_its_limit(dtype, most, h):
 def test_layouts_of_up_to_1024_heads():
     assert B.locret_paged_workspace_bytes(cfg(n_q_heads=1024, n_kv_heads=8)) > 0
     assert B.locret_paged_workspace_bytes(cfg(n_q_heads=1032, n_kv_heads=129)) == 0
+
+
+def test_a_ramp_that_does_not_extend_keeps_its_amplitude():
+    kw = dict(original=4096, low=1.0, high=32.0)
+    assert B.locret_rope_frequencies(64, 10000.0, B.LOCRET_ROPE_RAMP, factor=0.5, **kw)[1] == 1.0
+    f, a = B.locret_rope_frequencies(64, 10000.0, B.LOCRET_ROPE_RAMP, factor=1.0, **kw)
+    # the mixture k f + (1 - k) f of a pair: four roundings of numbers that add up to f, each off by at most 2^-53 of its own
+    assert a == 1.0 and all(math.isclose(x, y, rel_tol=2.0 ** -51) for x, y in zip(f, B.locret_rope_frequencies(64, 10000.0)[0]))
