@@ -250,8 +250,9 @@ int locret_profile_read(locret_ctx* ctx, double* stage_ms, int32_t* n_calls);
  *   lens          [n_req] int32: units of every request in the cache
  *   slot          page * page_size + place in the page, of one unit
  * A serving step is locret_paged_plan, then for every layer locret_paged_append and locret_paged_decode (every request has one new
- * token) or locret_paged_prefill (any other step: chunks, requests that wait or are finished).  The retained cache of a locret_ctx is moved into pages by
- * locret_paged_append too: its K and V (locret_cache_view) are read with head strides, rotated to positions 0, 1, ...
+ * token) or locret_paged_prefill (any other step: chunks, requests that wait or are finished).  The retained cache of a
+ * locret_ctx is moved into pages by locret_paged_append too: its K and V (locret_cache_view) are read with head strides, rotated to
+ * positions 0, 1, ...
  *
  * Conventions: those of the top of this file, except
  *   - calls carry their configuration (HOST) and workspace, and no state is kept between them: calls on different streams

@@ -1057,3 +1057,38 @@ def test_a_step_in_which_requests_wait_finish_or_are_not_served(dtype):
             close(dec[r: r + 1], want[-1:], tol[-1:], f"decode of request {r} of {new}")
         assert (dec[[r for r in range(6) if not streams[r][0].shape[0]]] == 0).all()
     assert at == [0, 10, 10, 50, 55, 55, 55]
+
+
+@pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("bf16", 64, 16), ("f32", 64, 16)])
+@pytest.mark.parametrize("window,sink", [(0, 0), (50, 4)])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_rows_with_a_logit_of_infinity_or_nan_are_nan(dtype, d, page, window, sink, value):
+    """Rows that see such a key, and no others."""
+    rng = np.random.default_rng(d + page + window)
+    lens, new = [700, 200, 90], [30, 200, 90]
+    c = paged_case(rng, dtype, 4, 2, d, page, lens, window, sink)
+    at = [(0, 690), (0, 100), (1, 60), (2, 0)]
+    for r, u in at:
+        c["K"][c["table"][r, u // page], :, u % page, 0] = value
+    q, q64 = numbers(rng, dtype, sum(new), 4, d)
+    q[..., 0] = 1.0
+    q64[..., 0] = 1.0
+    cu = np.cumsum([0] + new)
+    rows = [(r, i) for r in range(3) for i in range(new[r])]
+
+    def check(rows, out, lse, what):
+        for t, (r, i) in enumerate(rows):
+            see = R.visible(lens[r] - new[r] + i, lens[r], window, sink)
+            if any(see[u] for s, u in at if s == r):
+                assert np.isnan(out[t]).all() and np.isnan(lse[t]).all(), (what, r, i)
+                continue
+            for j in range(4):
+                K, V = (units(c, c[x], r, j // 2)[0] for x in ("K64", "V64"))
+                want, wl, tol, ltol = R.attend(q64[cu[r] + i, j], K, V, see, c["scale"], dtype)
+                assert (np.abs(out[t, j] - want) <= tol).all() and abs(lse[t, j] - wl) <= ltol, (what, r, i, j)
+
+    out, lse = run_prefill(c, q, cu)
+    check(rows, out, lse, "prefill")
+    last = cu[1:] - 1
+    out, lse = run_decode(c, q[torch.from_numpy(last).to(DEV)].contiguous())
+    check([(r, new[r] - 1) for r in range(3)], out, lse, "decode")
